@@ -60,6 +60,8 @@ extern "C" {
  * W[r][c] = scale[r] * q[r][c]; the embedding, the norm gains and the KV
  * cache are bf16.  Activations and accumulation stay fp32 as for DV_BF16. */
 #define DV_I8 2
+/* A code format of the 8-bit KV cache (dv_kvq), not a weight type: e4m3. */
+#define DV_F8 3
 
 #define DV_MAX_TREE 64
 
@@ -295,6 +297,114 @@ int dv_kv_commit(dv_handle *h, dv_kv *kv, const dv_accept *accept);
  * stream.  Errors: DV_EINVAL, DV_ECAPACITY, DV_EHIP. */
 int dv_prefill(dv_handle *h, const int32_t *tokens, int32_t n, dv_kv *kv,
                int32_t *out_next_token);
+
+/* ---- 8-bit KV cache ------------------------------------------------------
+ *
+ * A cache whose committed keys and values take one byte per number, with one
+ * fp32 scale for each block of 32 slots and KV head, K and V apart: value =
+ * scale * code, code int8 in [-127, 127] (format DV_I8) or e4m3 (DV_F8).  The
+ * slots behind the last whole block stay bf16 in a tail: up to 31 committed rows
+ * and the up to 64 new ones of a step behind them.  A row is quantised once, when
+ * its block is full, from its bf16 value, so the codes do not depend on how the
+ * tokens came (prompt, chains, accepted paths).
+ *
+ * A block with largest magnitude a is quantised with Q = 127 or 448:
+ *   a finite and >= 2^-100: scale = a / Q, factor = Q / a, code = x * factor
+ *     (each rounded to fp32), then to the nearest code, ties to even;
+ *   a < 2^-100: scale 0, codes 0;   an infinity or NaN in the block: scale NaN,
+ *     codes 0 (every number of the block reads back as NaN).
+ *
+ *   k, v:    codes [n_layers][n_heads][capacity / 32] blocks of 32 head_dim bytes.
+ *     K, slot s (0..31) and dim j: byte ((2 (j/64) + s/4%2) 64 + 16 (j%32/8) +
+ *       4 (s/8) + s%4) 16 + 8 (j%64/32) + j%8 of the block;
+ *     V: byte (64 (j/32) + 16 (s/8) + j%16) 16 + 8 (j%32/16) + s%8;
+ *   scale:   [n_layers][n_heads][capacity / 32][2], K's and V's;
+ *   k_tail:  bf16 [n_layers][n_heads][96][head_dim], v_tail: bf16
+ *     [n_layers][n_heads][3][head_dim][32] (dv_kv's layouts with capacity 96);
+ *     tail slot i is slot 32 (len / 32) + i of the sequence.
+ * All are device buffers of the caller, 16-byte aligned (scale: 8); they need not
+ * start at zero.  n_heads counts KV heads; head_dim is 64 or 128; capacity a
+ * positive multiple of 32.  len is host state: dv_kvq_store, dv_kvq_advance,
+ * dv_kvq_commit and dv_prefill_kvq advance it; 0 (nothing else) makes a cache
+ * empty. */
+#define DV_KVQ_TAIL 96
+typedef struct dv_kvq {
+    void *k;
+    void *v;
+    float *scale;
+    void *k_tail;
+    void *v_tail;
+    int32_t n_layers;
+    int32_t n_heads;
+    int32_t head_dim;
+    int32_t format; /* DV_I8 or DV_F8 */
+    int32_t capacity;
+    int32_t len;
+} dv_kvq;
+
+/* Operators on an 8-bit cache.  They need no handle, allocate nothing and do not
+ * synchronise: they queue their kernels on `stream` (a hipStream_t of the current
+ * device, NULL = default stream), which may be capturing.  The layouts, len and host
+ * arrays are read during the call, so a captured call repeats with the len that it
+ * was captured with.  Calls on different caches may run at once; calls on one cache
+ * must be ordered, and a call that changes a cache must not run while another reads
+ * it.  Errors (message via dv_last_error(NULL)): DV_EINVAL, DV_ECAPACITY, DV_EHIP. */
+
+/* Append rows [len, len + n) of a bf16 cache of the same layers, heads and head_dim
+ * (committed there: kv->len >= len + n): whole blocks are quantised, the rest goes
+ * to the tail; len += n. */
+int dv_kvq_store(dv_kvq *kvq, const dv_kv *kv, int32_t n, void *stream);
+
+/* Read all len rows back into a bf16 cache of the same layers, heads and head_dim:
+ * scale * code rounded to fp32 and to bf16, tail rows as they are; kv->len = len.
+ * Slots from len on keep what they hold. */
+int dv_kvq_load(const dv_kvq *kvq, dv_kv *kv, void *stream);
+
+/* New rows become committed: tail row len % 32 + path[i] moves to slot len + i, i <
+ * n (path: HOST array, increasing, 0 <= path[i] < 64), blocks that are full are
+ * quantised and the tail moves up; len += n.  This is dv_kvq_commit without a step:
+ * for a caller that keeps its own tree. */
+int dv_kvq_advance(dv_kvq *kvq, const int32_t *path, int32_t n, void *stream);
+
+/* Attention of n new rows (1..64) over layer `layer`: the keys are the len
+ * committed ones and the new rows themselves, in tail slots len % 32 + i (where
+ * dv_verify_step_kvq's projections put them; a caller of its own writes them there).
+ *   out[i][h] = sum_j softmax_j(q[i][h] . k_j / sqrt(head_dim)) v_j
+ * over the committed slots and the new rows j whose bit j of mask[i] is set
+ * (dv_tree_prepare's out_anc; NULL: row i sees rows 0..i).  A row that sees nothing
+ * gives zeros.  Scores, softmax and sums are fp32.
+ *   q, out: device fp32 [n][n_heads][head_dim], rows q_stride and out_stride floats
+ *     apart (multiples of 4, at least n_heads head_dim), 16-byte aligned.  n_heads is
+ *     a multiple of kvq->n_heads: query heads h with the same h / (n_heads /
+ *     kvq->n_heads) share a KV head;
+ *   mask: HOST array of n;
+ *   workspace: device memory, 16-byte aligned, of at least
+ *     dv_kvq_attention_workspace(kvq, n, n_heads) bytes (enough for any len of this
+ *     capacity on this device; it may be 0, and workspace NULL).  Its contents do not
+ *     matter before or after.  Calls that may run at once, captured ones included,
+ *     need one each. */
+int dv_kvq_attention(const dv_kvq *kvq, int32_t layer, const float *q, int64_t q_stride, int32_t n, int32_t n_heads,
+                     const uint64_t *mask, float *out, int64_t out_stride, void *workspace, int64_t workspace_bytes,
+                     void *stream);
+/* Bytes of workspace, or a negative error. */
+int64_t dv_kvq_attention_workspace(const dv_kvq *kvq, int32_t n, int32_t n_heads);
+
+/* dv_verify_step, dv_verify_step_sampled, dv_prefill and dv_kv_commit over an 8-bit
+ * cache (bf16 or int8 weights; n_layers, n_heads and head_dim are the model's).
+ * Committed keys and values enter as scale * code, a step's or chain's own and the
+ * tail's as bf16.  A prompt on the causal pass reads each layer back into one layer of
+ * bf16 rows that the handle allocates at the first such prompt (4 d_model bytes per
+ * slot), extends it there and appends the new rows; a chunk's own keys (up to 1024
+ * tokens) enter as bf16.  Errors as theirs; DV_EINVAL too for fp32 weights or another
+ * model's cache, and a step is committed by the call of its own kind only
+ * (DV_ESTATE). */
+int dv_verify_step_kvq(dv_handle *h, const int32_t *tokens, const int32_t *tree_parents, int32_t n_tree,
+                       dv_kvq *kvq, float *out_logits, dv_accept *out_accept);
+int dv_verify_step_kvq_sampled(dv_handle *h, const int32_t *tokens, const int32_t *tree_parents, int32_t n_tree,
+                               dv_kvq *kvq, const float *draft_probs, float temperature, const float *u_accept,
+                               const float *u_bonus, float *out_logits, dv_accept *out_accept);
+int dv_prefill_kvq(dv_handle *h, const int32_t *tokens, int32_t n, dv_kvq *kvq, int32_t *out_next_token);
+int dv_kvq_commit(dv_handle *h, dv_kvq *kvq, const dv_accept *accept);
 
 /* Release the handle and its workspace (NULL is ignored). */
 void dv_verify_free(dv_handle *h);

@@ -9,7 +9,7 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libdv.so")
-SOURCES = ["dv_kernels.hip", "dv_prefill.hip", "dv_engine.cpp"]
+SOURCES = ["dv_kernels.hip", "dv_prefill.hip", "dv_kvq.hip", "dv_engine.cpp", "dv_kvq.cpp"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -11,112 +11,11 @@
 #include <string>
 #include <vector>
 
-#include "dv.h"
-#include "dv_internal.h"
+#include "dv_engine.h"
 
 namespace {
-
 thread_local std::string g_init_error;
-
-struct LayerW {
-    const void *attn_norm, *wq, *wk, *wv, *wo, *ffn_norm, *w_gate, *w_up, *w_down;
-    const float *sq = nullptr, *sk = nullptr, *sv = nullptr, *so = nullptr, *sg = nullptr, *su = nullptr,
-                *sd = nullptr;  // int8: row scales as passed in
-    uint16_t *pk_qkv = nullptr, *pk_o = nullptr, *pk_gu = nullptr, *pk_down = nullptr;
-    float *ps_qkv = nullptr, *ps_o = nullptr, *ps_gu = nullptr, *ps_down = nullptr;  // int8: packed-order scales
-};
-
-struct GemmPlan {
-    int n_tiles = 0;   // 32-row tiles
-    int mfma = 0;      // packed weights and split-layout activations (bf16 and int8 weights, K % 32 == 0)
-    int rb = 0;        // 16-row blocks per row group (0: the VALU kernel)
-    int n_groups = 0;  // row groups (VALU: tiles)
-    int ks = 1;        // K splits per row group (residual projections)
-};
-
-struct ProfEv {
-    int cls;
-    hipEvent_t a, b;
-};
-
-}  // namespace
-
-struct dv_handle {
-    dv_config cfg{};
-    hipStream_t stream = nullptr;
-    int bf16 = 0;          // 16-bit embedding, gains and KV cache; MFMA projections
-    int wkind = W_F32;     // projection weights: W_F32, W_BF16 or W_I8
-    size_t esz = 4;
-    const void *embed = nullptr, *final_norm = nullptr, *lm_head = nullptr;
-    std::vector<LayerW> layers;
-
-    // workspace (device)
-    float *x = nullptr, *u = nullptr, *q = nullptr, *attn = nullptr, *hbuf = nullptr;
-    float *ssq = nullptr;  // per-token partial sums of squares, [64][ssq_max]
-    int ssq_max = 0;
-    float *part_gemm = nullptr;  // split-K partials of the residual projections
-    uint32_t *cnt = nullptr;     // their per-row-group arrival counters
-    size_t part_elems = 0;       // floats in part_gemm
-    int cnt_n = 0;               // counters in cnt
-    uint16_t *u_s = nullptr, *attn_s = nullptr, *h_s = nullptr;  // split-layout activations
-    float *part_o = nullptr, *part_m = nullptr, *part_l = nullptr;
-    uint32_t *attn_cnt = nullptr;  // per-head arrivals of the attention splits
-    int attn_split_max = 0;
-    float *arg_val = nullptr;
-    int32_t *arg_idx = nullptr;
-    float *rope_cos = nullptr, *rope_sin = nullptr;
-    uint16_t *pk_lm = nullptr;
-    const float *lm_scale = nullptr;
-    float *ps_lm = nullptr;
-    StepDesc *h_sd = nullptr;  // the step's tree (kernels get it by value)
-    DevAccept *d_acc = nullptr, *h_acc = nullptr;  // one pinned host struct, as the device and the host address it
-    float *logits_ws = nullptr;  // [max_tree][vocab] logits of a sampled step without out_logits
-    // large-M prefill (allocated at its first use, sized for pf_cap tokens,
-    // a multiple of 128; pf_part and pf_cnt for the split-K units of any
-    // chunk of up to that many): residual stream, rotated queries, the split-layout
-    // operands (norm numerators, attention output, SwiGLU output) and the
-    // norms' sums of squares over 64-row slices
-    int pf_cap = 0;
-    void *pf_block = nullptr;  // the allocation that holds them all
-    int32_t *pf_tok = nullptr;
-    float *pf_x = nullptr, *pf_q = nullptr, *pf_ssq = nullptr;
-    uint16_t *pf_us = nullptr, *pf_as = nullptr, *pf_hs = nullptr;
-    float *pf_part = nullptr;
-    uint32_t *pf_cnt = nullptr;
-    // draft side
-    bool draft = false;
-    const void *dgf_h = nullptr, *dgf_e = nullptr, *dgf_g = nullptr;  // W_h, W_e [d][d], W_g [d][2d]
-    GemmPlan p_dgf_d, p_dgf_g;    // projections of W_h / W_e (K = d) and W_g (K = 2 d)
-    uint16_t *pk_dh = nullptr, *pk_de = nullptr, *pk_dg = nullptr;  // their MFMA block order
-    uint16_t *dgf_xf = nullptr, *dgf_xe = nullptr, *dgf_xg = nullptr;  // split-layout operands
-    float *dgf_h1 = nullptr, *dgf_h2 = nullptr, *dgf_z = nullptr;       // [64][d] outputs
-    const float *x_in = nullptr;  // stack input rows for the next forward (null: embeddings)
-    float *feat_a = nullptr, *feat_b = nullptr;  // [DV_TREE_MAX + 1][d] draft features (row 64: the root's input)
-    int32_t *tk_tok = nullptr, *tk_tok_h = nullptr;
-    float *tk_p = nullptr, *tk_p_h = nullptr;
-    float *p_ws = nullptr;       // [2][vocab] current / residual distribution of the one-workgroup sampling walk
-    GemmPlan p_qkv, p_o, p_gu, p_down, p_lm;
-    int n_cu = 256;
-
-    // pending (uncommitted) step
-    bool pending = false;
-    int32_t pend_n = 0, pend_base = 0;
-    int32_t pend_parents[DV_TREE_MAX];
-    void *pend_k = nullptr, *pend_v = nullptr;
-
-    bool poisoned = false;
-    std::string err;
-
-    // per-kernel-class event timing
-    int prof = 0;  // class mask
-    bool prof_open = false;
-    std::vector<hipEvent_t> ev_pool;
-    std::vector<ProfEv> ev_live;
-    double prof_ms[DV_K_COUNT] = {0, 0, 0, 0};
-    int64_t prof_n[DV_K_COUNT] = {0, 0, 0, 0};
-};
-
-namespace {
+}
 
 int set_err(dv_handle *h, int code, const char *fmt, ...)
 {
@@ -135,6 +34,8 @@ int hip_fail(dv_handle *h, hipError_t e, const char *what)
     if (h) h->poisoned = true;
     return set_err(h, DV_EHIP, "HIP error in %s: %s", what, hipGetErrorString(e));
 }
+
+namespace {
 
 #define HIPCHK(h, call)                                        \
     do {                                                       \
@@ -279,8 +180,9 @@ int check_tree(dv_handle *h, const int32_t *parents, int n, int base, int32_t *p
 // (the greedy rule, or the sampling rule when smp is given; out_logits must
 // then be non-null, and smp's logits are set to it).
 int enqueue_forward(dv_handle *h, const dv_kv *kv, float *out_logits, bool with_head,
-                    SampleArgs *smp = nullptr)
+                    SampleArgs *smp = nullptr, CacheSeam *seam = nullptr)
 {
+    if (seam) kv = &seam->rows;
     const dv_config &c = h->cfg;
     StepDesc *sd = h->h_sd;
     const int M = sd->M, Mpad = sd->Mpad, P = sd->P, half = sd->half;
@@ -304,7 +206,7 @@ int enqueue_forward(dv_handle *h, const dv_kv *kv, float *out_logits, bool with_
     g.Mpad = Mpad;
     g.half = half;
     g.cap = kv->capacity;
-    g.P = P;
+    g.P = seam ? seam->slot : P;
     g.hd = hd;
     g.rope_cos = h->rope_cos;
     g.rope_sin = h->rope_sin;
@@ -430,7 +332,7 @@ int enqueue_forward(dv_handle *h, const dv_kv *kv, float *out_logits, bool with_
         aa.kc = g.kc;
         aa.vc = g.vc;
         prof_begin(h, DV_K_ATTN);
-        hipError_t e = launch_attention(aa, h->bf16, s);
+        hipError_t e = seam ? seam->attend(aa, l) : launch_attention(aa, h->bf16, s);
         prof_end(h);
         if (e != hipSuccess) return hip_fail(h, e, "attention launch");
         if ((rc = gemm(h->p_o, EPI_RESID, w.wo, nullptr, nullptr, w.pk_o, w.ps_o, d, d, h->attn, h->attn_s, nullptr,
@@ -663,14 +565,16 @@ int pf_reserve(dv_handle *h, int tokens, bool split)
 }
 
 // (the workspace is reserved)
-int prefill_large(dv_handle *h, const int32_t *tokens, int n, dv_kv *kv, int32_t *out_next_token)
+int prefill_large(dv_handle *h, const int32_t *tokens, int n, dv_kv *kv, int32_t *out_next_token,
+                  CacheSeam *seam = nullptr)
 {
+    const dv_kv *at = seam ? &seam->rows : kv;  // where the keys and values are written and read
     const dv_config &c = h->cfg;
     const int d = c.d_model, F = c.d_ffn, H = c.n_heads, hd = c.head_dim;
     hipStream_t s = h->stream;
     int rc;
     auto ck = [&](hipError_t e, const char *what) -> int { return e == hipSuccess ? DV_OK : hip_fail(h, e, what); };
-    const size_t layer_kv = (size_t)H * kv->capacity * hd;
+    const size_t layer_kv = seam ? 0 : (size_t)H * kv->capacity * hd;
     const bool q8 = h->wkind == W_I8;
     int done = 0;
     while (done < n) {
@@ -694,7 +598,7 @@ int prefill_large(dv_handle *h, const int32_t *tokens, int n, dv_kv *kv, int32_t
         base.eps = c.rms_eps;
         base.d = d;
         base.q = h->pf_q;
-        base.cap = kv->capacity;
+        base.cap = at->capacity;
         base.hd = hd;
         base.rope_cos = h->rope_cos;
         base.rope_sin = h->rope_sin;
@@ -721,14 +625,16 @@ int prefill_large(dv_handle *h, const int32_t *tokens, int n, dv_kv *kv, int32_t
         };
         for (int l = 0; l < c.n_layers; ++l) {
             const LayerW &w = h->layers[l];
-            base.kc = static_cast<uint16_t *>(kv->k) + (size_t)l * layer_kv;
-            base.vc = static_cast<uint16_t *>(kv->v) + (size_t)l * layer_kv;
+            base.kc = static_cast<uint16_t *>(at->k) + (size_t)l * layer_kv;
+            base.vc = static_cast<uint16_t *>(at->v) + (size_t)l * layer_kv;
+            if (seam && (rc = ck(seam->before(l, M), "cache read-back"))) return rc;
             if ((rc = gemm(plan.qkv, EPI_QKV, w.pk_qkv, w.ps_qkv, 3 * d, d, h->pf_us, nullptr))) return rc;
             prof_begin(h, DV_K_ATTN);
-            rc = ck(launch_attn_causal(h->pf_q, base.kc, base.vc, M, P0, H, hd, kv->capacity, MT, h->n_cu, h->pf_as, s),
+            rc = ck(launch_attn_causal(h->pf_q, base.kc, base.vc, M, P0, H, hd, at->capacity, MT, h->n_cu, h->pf_as, s),
                     "causal attention");
             prof_end(h);
             if (rc) return rc;
+            if (seam && (rc = ck(seam->after(l, M), "cache store"))) return rc;
             if ((rc = gemm(plan.o, EPI_RESID, w.pk_o, w.ps_o, d, d, h->pf_as, w.ffn_norm))) return rc;
             if ((rc = gemm(plan.gu, EPI_SWIGLU, w.pk_gu, w.ps_gu, 2 * F, d, h->pf_us, nullptr))) return rc;
             const void *next_gain = l + 1 < c.n_layers ? h->layers[l + 1].attn_norm : h->final_norm;
@@ -796,6 +702,7 @@ int prefill_large(dv_handle *h, const int32_t *tokens, int n, dv_kv *kv, int32_t
         HIPCHK(h, hipStreamSynchronize(s));  // also keeps the token upload alive until used
         prof_collect(h);
         kv->len += M;
+        if (seam) seam->chunk_done(M);
         done += M;
         if (last && out_next_token) *out_next_token = h->h_acc->argmax[0];
     }
@@ -876,6 +783,128 @@ int check_kv(dv_handle *h, const dv_kv *kv)
 }
 
 }  // namespace
+
+int verify_step_impl(dv_handle *h, const int32_t *tokens, const int32_t *tree_parents, int32_t n_tree, dv_kv *kv,
+                     float *out_logits, dv_accept *out_accept, const float *draft_probs, float temperature,
+                     const float *u_accept, const float *u_bonus, bool sampled, CacheSeam *seam)
+{
+    if (!h) return set_err(nullptr, DV_EINVAL, "null handle");
+    if (h->poisoned) return DV_EHIP;
+    if (!tokens || !tree_parents || !out_accept) return set_err(h, DV_EINVAL, "null argument");
+    int rc = check_kv(h, kv);
+    if (rc) return rc;
+    if (n_tree < 1 || n_tree > h->cfg.max_tree)
+        return set_err(h, DV_EINVAL, "n_tree %d outside [1, %d]", n_tree, h->cfg.max_tree);
+    for (int i = 0; i < n_tree; ++i)
+        if (tokens[i] < 0 || tokens[i] >= h->cfg.vocab)
+            return set_err(h, DV_EINVAL, "token id %d at node %d outside [0, %d)", tokens[i], i, h->cfg.vocab);
+    int32_t pos[DV_MAX_TREE], depth[DV_MAX_TREE];
+    uint64_t anc[DV_MAX_TREE];
+    if ((rc = check_tree(h, tree_parents, n_tree, kv->len, pos, depth, anc))) return rc;
+    if ((long)kv->len + n_tree > kv->capacity || (long)kv->len + n_tree > h->cfg.max_ctx)
+        return set_err(h, DV_ECAPACITY, "len %d + n_tree %d exceeds capacity %d / max_ctx %d",
+                       kv->len, n_tree, kv->capacity, h->cfg.max_ctx);
+    SampleArgs sa;
+    if (sampled) {
+        if ((rc = prepare_sampled(h, tokens, tree_parents, n_tree, h->cfg.vocab, draft_probs, temperature, u_accept, u_bonus,
+                                  h->p_ws, h->d_acc,
+                                  &sa)))
+            return rc;
+        if (out_logits && reinterpret_cast<uintptr_t>(out_logits) % 16)
+            return set_err(h, DV_EINVAL, "out_logits must be 16-byte aligned");
+        if (!out_logits) out_logits = h->logits_ws;
+    }
+
+    fill_desc(h->h_sd, tokens, tree_parents, n_tree, kv->len, pos, depth, anc);
+    if ((rc = enqueue_forward(h, kv, out_logits, true, sampled ? &sa : nullptr, seam))) return rc;
+    HIPCHK(h, hipStreamSynchronize(h->stream));
+    prof_collect(h);
+
+    if (sampled && sample_by_node(h->cfg.vocab)) walk_sampled(h->h_acc);
+    const DevAccept &a = *h->h_acc;
+    std::memset(out_accept, 0, sizeof *out_accept);
+    out_accept->accept_len = a.accept_len;
+    out_accept->bonus_token = a.bonus;
+    out_accept->n_tree = n_tree;
+    out_accept->base_len = kv->len;
+    for (int i = 0; i < a.accept_len && i < DV_MAX_TREE; ++i) out_accept->path[i] = a.path[i];
+    if (!sampled)
+        for (int i = 0; i < n_tree; ++i) out_accept->argmax[i] = a.argmax[i];
+
+    h->pending = true;
+    h->pend_n = n_tree;
+    h->pend_base = kv->len;
+    h->pend_k = kv->k;
+    h->pend_v = kv->v;
+    h->pend_kvq = seam != nullptr;
+    std::memcpy(h->pend_parents, tree_parents, n_tree * sizeof(int32_t));
+    return DV_OK;
+}
+
+int check_commit(dv_handle *h, const dv_kv *kv, const dv_accept *acc, bool kvq, bool *identity)
+{
+    if (!h->pending) return set_err(h, DV_ESTATE, "no pending verification step to commit");
+    if (kvq != h->pend_kvq || acc->n_tree != h->pend_n || acc->base_len != h->pend_base || kv->len != h->pend_base ||
+        kv->k != h->pend_k || kv->v != h->pend_v)
+        return set_err(h, DV_ESTATE, "accept struct or cache does not match the pending step");
+    const int n = acc->accept_len;
+    if (n < 1 || n > h->pend_n) return set_err(h, DV_EINVAL, "accept_len %d outside [1, %d]", n, h->pend_n);
+    if (acc->path[0] != 0) return set_err(h, DV_EINVAL, "path must start at the root");
+    *identity = true;
+    for (int k = 1; k < n; ++k) {
+        const int node = acc->path[k];
+        if (node <= acc->path[k - 1] || node >= h->pend_n || h->pend_parents[node] != acc->path[k - 1])
+            return set_err(h, DV_EINVAL, "path is not a root-to-node chain of the pending tree");
+        if (node != k) *identity = false;
+    }
+    return DV_OK;
+}
+
+int prefill_impl(dv_handle *h, const int32_t *tokens, int32_t n, dv_kv *kv, int32_t *out_next_token, CacheSeam *seam)
+{
+    if (!h) return set_err(nullptr, DV_EINVAL, "null handle");
+    if (h->poisoned) return DV_EHIP;
+    if (!tokens || n < 1) return set_err(h, DV_EINVAL, "empty prompt");
+    int rc = check_kv(h, kv);
+    if (rc) return rc;
+    for (int i = 0; i < n; ++i)
+        if (tokens[i] < 0 || tokens[i] >= h->cfg.vocab)
+            return set_err(h, DV_EINVAL, "token id %d at %d outside [0, %d)", tokens[i], i, h->cfg.vocab);
+    if ((long)kv->len + n > kv->capacity || (long)kv->len + n > h->cfg.max_ctx)
+        return set_err(h, DV_ECAPACITY, "prompt of %d does not fit (len %d, capacity %d, max_ctx %d)",
+                       n, kv->len, kv->capacity, h->cfg.max_ctx);
+    if (pf_supported(h) && n > h->cfg.max_tree && !chains_faster(h, n, kv->len)) {
+        // without room for its workspace the prompt runs as chains, which need none
+        rc = pf_reserve(h, std::min(n, DV_PF_CHUNK), true);
+        if (rc == DV_OK && seam) rc = seam->reserve(kv->len + n);
+        if (rc == DV_OK) {
+            rc = prefill_large(h, tokens, n, kv, out_next_token, seam);
+            h->pending = false;
+        }
+        if (rc != DV_ENOMEM) return rc;
+    }
+    const int chunk = h->cfg.max_tree;
+    int32_t parents[DV_MAX_TREE], pos[DV_MAX_TREE], depth[DV_MAX_TREE];
+    uint64_t anc[DV_MAX_TREE];
+    for (int i = 0; i < DV_MAX_TREE; ++i) parents[i] = i - 1;
+    int done = 0;
+    while (done < n) {
+        const int c = std::min(chunk, n - done);
+        const bool last = done + c == n;
+        if ((rc = check_tree(h, parents, c, kv->len, pos, depth, anc))) return rc;
+        fill_desc(h->h_sd, tokens + done, parents, c, kv->len, pos, depth, anc);
+        if ((rc = enqueue_forward(h, kv, nullptr, last, nullptr, seam))) return rc;
+        hipError_t e = seam ? seam->committed(c) : hipSuccess;
+        if (e != hipSuccess) return hip_fail(h, e, "cache advance launch");
+        HIPCHK(h, hipStreamSynchronize(h->stream));
+        prof_collect(h);
+        kv->len += c;  // a chain's nodes already sit at slots len + k
+        done += c;
+        if (last && out_next_token) *out_next_token = h->h_acc->argmax[c - 1];
+    }
+    h->pending = false;
+    return DV_OK;
+}
 
 extern "C" {
 
@@ -1124,67 +1153,11 @@ int dv_verify_init(const dv_config *cfg, const dv_weights *w, void *stream, dv_h
     return DV_OK;
 }
 
-static int verify_step_impl(dv_handle *h, const int32_t *tokens, const int32_t *tree_parents, int32_t n_tree,
-                            dv_kv *kv, float *out_logits, dv_accept *out_accept, const float *draft_probs,
-                            float temperature, const float *u_accept, const float *u_bonus, bool sampled)
-{
-    if (!h) return set_err(nullptr, DV_EINVAL, "null handle");
-    if (h->poisoned) return DV_EHIP;
-    if (!tokens || !tree_parents || !out_accept) return set_err(h, DV_EINVAL, "null argument");
-    int rc = check_kv(h, kv);
-    if (rc) return rc;
-    if (n_tree < 1 || n_tree > h->cfg.max_tree)
-        return set_err(h, DV_EINVAL, "n_tree %d outside [1, %d]", n_tree, h->cfg.max_tree);
-    for (int i = 0; i < n_tree; ++i)
-        if (tokens[i] < 0 || tokens[i] >= h->cfg.vocab)
-            return set_err(h, DV_EINVAL, "token id %d at node %d outside [0, %d)", tokens[i], i, h->cfg.vocab);
-    int32_t pos[DV_MAX_TREE], depth[DV_MAX_TREE];
-    uint64_t anc[DV_MAX_TREE];
-    if ((rc = check_tree(h, tree_parents, n_tree, kv->len, pos, depth, anc))) return rc;
-    if ((long)kv->len + n_tree > kv->capacity || (long)kv->len + n_tree > h->cfg.max_ctx)
-        return set_err(h, DV_ECAPACITY, "len %d + n_tree %d exceeds capacity %d / max_ctx %d",
-                       kv->len, n_tree, kv->capacity, h->cfg.max_ctx);
-    SampleArgs sa;
-    if (sampled) {
-        if ((rc = prepare_sampled(h, tokens, tree_parents, n_tree, h->cfg.vocab, draft_probs, temperature, u_accept, u_bonus,
-                                  h->p_ws, h->d_acc,
-                                  &sa)))
-            return rc;
-        if (out_logits && reinterpret_cast<uintptr_t>(out_logits) % 16)
-            return set_err(h, DV_EINVAL, "out_logits must be 16-byte aligned");
-        if (!out_logits) out_logits = h->logits_ws;
-    }
-
-    fill_desc(h->h_sd, tokens, tree_parents, n_tree, kv->len, pos, depth, anc);
-    if ((rc = enqueue_forward(h, kv, out_logits, true, sampled ? &sa : nullptr))) return rc;
-    HIPCHK(h, hipStreamSynchronize(h->stream));
-    prof_collect(h);
-
-    if (sampled && sample_by_node(h->cfg.vocab)) walk_sampled(h->h_acc);
-    const DevAccept &a = *h->h_acc;
-    std::memset(out_accept, 0, sizeof *out_accept);
-    out_accept->accept_len = a.accept_len;
-    out_accept->bonus_token = a.bonus;
-    out_accept->n_tree = n_tree;
-    out_accept->base_len = kv->len;
-    for (int i = 0; i < a.accept_len && i < DV_MAX_TREE; ++i) out_accept->path[i] = a.path[i];
-    if (!sampled)
-        for (int i = 0; i < n_tree; ++i) out_accept->argmax[i] = a.argmax[i];
-
-    h->pending = true;
-    h->pend_n = n_tree;
-    h->pend_base = kv->len;
-    h->pend_k = kv->k;
-    h->pend_v = kv->v;
-    std::memcpy(h->pend_parents, tree_parents, n_tree * sizeof(int32_t));
-    return DV_OK;
-}
-
 int dv_verify_step(dv_handle *h, const int32_t *tokens, const int32_t *tree_parents, int32_t n_tree,
                    dv_kv *kv, float *out_logits, dv_accept *out_accept)
 {
     return verify_step_impl(h, tokens, tree_parents, n_tree, kv, out_logits, out_accept, nullptr, 0.f, nullptr,
-                            nullptr, false);
+                            nullptr, false, nullptr);
 }
 
 int dv_verify_step_sampled(dv_handle *h, const int32_t *tokens, const int32_t *tree_parents, int32_t n_tree,
@@ -1192,7 +1165,7 @@ int dv_verify_step_sampled(dv_handle *h, const int32_t *tokens, const int32_t *t
                            const float *u_bonus, float *out_logits, dv_accept *out_accept)
 {
     return verify_step_impl(h, tokens, tree_parents, n_tree, kv, out_logits, out_accept, draft_probs,
-                            temperature, u_accept, u_bonus, true);
+                            temperature, u_accept, u_bonus, true, nullptr);
 }
 
 int dv_accept_sampled(dv_handle *h, const float *logits, const int32_t *tokens, const int32_t *tree_parents,
@@ -1506,20 +1479,9 @@ int dv_kv_commit(dv_handle *h, dv_kv *kv, const dv_accept *acc)
     if (!acc) return set_err(h, DV_EINVAL, "null accept struct");
     int rc = check_kv(h, kv);
     if (rc) return rc;
-    if (!h->pending) return set_err(h, DV_ESTATE, "no pending verification step to commit");
-    if (acc->n_tree != h->pend_n || acc->base_len != h->pend_base || kv->len != h->pend_base ||
-        kv->k != h->pend_k || kv->v != h->pend_v)
-        return set_err(h, DV_ESTATE, "accept struct or cache does not match the pending step");
+    bool identity;
+    if ((rc = check_commit(h, kv, acc, false, &identity))) return rc;
     const int n = acc->accept_len;
-    if (n < 1 || n > h->pend_n) return set_err(h, DV_EINVAL, "accept_len %d outside [1, %d]", n, h->pend_n);
-    if (acc->path[0] != 0) return set_err(h, DV_EINVAL, "path must start at the root");
-    bool identity = true;
-    for (int k = 1; k < n; ++k) {
-        const int node = acc->path[k];
-        if (node <= acc->path[k - 1] || node >= h->pend_n || h->pend_parents[node] != acc->path[k - 1])
-            return set_err(h, DV_EINVAL, "path is not a root-to-node chain of the pending tree");
-        if (node != k) identity = false;
-    }
     if (!identity) {
         CommitArgs ca{};
         ca.kc = kv->k;
@@ -1540,45 +1502,7 @@ int dv_kv_commit(dv_handle *h, dv_kv *kv, const dv_accept *acc)
 
 int dv_prefill(dv_handle *h, const int32_t *tokens, int32_t n, dv_kv *kv, int32_t *out_next_token)
 {
-    if (!h) return set_err(nullptr, DV_EINVAL, "null handle");
-    if (h->poisoned) return DV_EHIP;
-    if (!tokens || n < 1) return set_err(h, DV_EINVAL, "empty prompt");
-    int rc = check_kv(h, kv);
-    if (rc) return rc;
-    for (int i = 0; i < n; ++i)
-        if (tokens[i] < 0 || tokens[i] >= h->cfg.vocab)
-            return set_err(h, DV_EINVAL, "token id %d at %d outside [0, %d)", tokens[i], i, h->cfg.vocab);
-    if ((long)kv->len + n > kv->capacity || (long)kv->len + n > h->cfg.max_ctx)
-        return set_err(h, DV_ECAPACITY, "prompt of %d does not fit (len %d, capacity %d, max_ctx %d)",
-                       n, kv->len, kv->capacity, h->cfg.max_ctx);
-    if (pf_supported(h) && n > h->cfg.max_tree && !chains_faster(h, n, kv->len)) {
-        // without room for its workspace the prompt runs as chains, which need none
-        rc = pf_reserve(h, std::min(n, DV_PF_CHUNK), true);
-        if (rc == DV_OK) {
-            rc = prefill_large(h, tokens, n, kv, out_next_token);
-            h->pending = false;
-        }
-        if (rc != DV_ENOMEM) return rc;
-    }
-    const int chunk = h->cfg.max_tree;
-    int32_t parents[DV_MAX_TREE], pos[DV_MAX_TREE], depth[DV_MAX_TREE];
-    uint64_t anc[DV_MAX_TREE];
-    for (int i = 0; i < DV_MAX_TREE; ++i) parents[i] = i - 1;
-    int done = 0;
-    while (done < n) {
-        const int c = std::min(chunk, n - done);
-        const bool last = done + c == n;
-        if ((rc = check_tree(h, parents, c, kv->len, pos, depth, anc))) return rc;
-        fill_desc(h->h_sd, tokens + done, parents, c, kv->len, pos, depth, anc);
-        if ((rc = enqueue_forward(h, kv, nullptr, last))) return rc;
-        HIPCHK(h, hipStreamSynchronize(h->stream));
-        prof_collect(h);
-        kv->len += c;  // a chain's nodes already sit at slots len + k
-        done += c;
-        if (last && out_next_token) *out_next_token = h->h_acc->argmax[c - 1];
-    }
-    h->pending = false;
-    return DV_OK;
+    return prefill_impl(h, tokens, n, kv, out_next_token, nullptr);
 }
 
 void dv_verify_free(dv_handle *h)
@@ -1605,6 +1529,7 @@ void dv_verify_free(dv_handle *h)
     if (h->tk_tok_h) (void)hipHostFree(h->tk_tok_h);
     if (h->tk_p_h) (void)hipHostFree(h->tk_p_h);
     if (h->pf_block) (void)hipFree(h->pf_block);
+    if (h->kvq_rows) (void)hipFree(h->kvq_rows);
     delete h->h_sd;
     if (h->h_acc) (void)hipHostFree(h->h_acc);
     for (auto &e : h->ev_live) { (void)hipEventDestroy(e.a); (void)hipEventDestroy(e.b); }

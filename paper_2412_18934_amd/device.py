@@ -1,4 +1,4 @@
-"""Device memory for the C ABI: weights, KV cache and outputs as torch tensors.
+"""Device memory for the C ABI: weights, KV caches and outputs as torch tensors.
 
 PyTorch is used only to allocate HIP device memory and copy host arrays into
 it; the tensors' raw addresses are handed to libdv.so.  Host arrays are numpy:
@@ -119,3 +119,34 @@ class DeviceKV:
                 return t.view(torch.int16).numpy().view(np.uint16)
             return t.numpy()
         return host(self.k[l, :, :n]), host(self._v_slots(l)[:, :n])
+
+
+class DeviceKVQ:
+    """8-bit KV cache (dv_kvq): codes and scales of whole 32-slot blocks, and the
+    bf16 tail behind them.  fmt: "i8" or "f8" (e4m3); n_heads counts KV heads."""
+
+    def __init__(self, n_layers, n_heads, head_dim, capacity, fmt="i8", device="cuda:0"):
+        codes = (n_layers, n_heads, capacity // 32, 32 * head_dim)
+        self.k = torch.zeros(codes, dtype=torch.int8, device=device)
+        self.v = torch.zeros(codes, dtype=torch.int8, device=device)
+        self.scale = torch.zeros(codes[:3] + (2,), dtype=torch.float32, device=device)
+        self.k_tail = torch.zeros((n_layers, n_heads, dv.DV_KVQ_TAIL, head_dim), dtype=torch.bfloat16, device=device)
+        self.v_tail = torch.zeros((n_layers, n_heads, dv.DV_KVQ_TAIL // 32, head_dim, 32), dtype=torch.bfloat16,
+                                  device=device)
+        self.c = dv.dv_kvq(self.k.data_ptr(), self.v.data_ptr(), self.scale.data_ptr(), self.k_tail.data_ptr(),
+                           self.v_tail.data_ptr(), n_layers, n_heads, head_dim, {"i8": dv.DV_I8, "f8": dv.DV_F8}[fmt],
+                           capacity, 0)
+
+    @property
+    def len(self) -> int:
+        return int(self.c.len)
+
+    def set_new(self, l: int, k: torch.Tensor, v: torch.Tensor):
+        """Put new rows k, v [n][n_heads][head_dim] of layer l behind the committed
+        ones, where dv_kvq_attention looks for them."""
+        at = torch.arange(self.len % 32, self.len % 32 + k.shape[0], device=self.k.device)
+        self.k_tail[l][:, at] = k.transpose(0, 1).to(torch.bfloat16)
+        self.v_tail[l][:, at // 32, :, at % 32] = v.to(torch.bfloat16)
+
+    def nbytes(self) -> int:
+        return sum(t.nbytes for t in (self.k, self.v, self.scale, self.k_tail, self.v_tail))

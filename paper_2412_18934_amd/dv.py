@@ -15,9 +15,10 @@ import numpy as np
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libdv.so")
 
 DV_OK, DV_EINVAL, DV_ECAPACITY, DV_ESTATE, DV_EHIP, DV_ENOMEM = 0, -1, -2, -3, -4, -5
-DV_F32, DV_BF16, DV_I8 = 0, 1, 2
+DV_F32, DV_BF16, DV_I8, DV_F8 = 0, 1, 2, 3
 DV_MAX_TREE = 64
 DV_NOALLOC_MAX_VOCAB = 262144
+DV_KVQ_TAIL = 96
 DV_K_GEMM, DV_K_ATTN, DV_K_NORM, DV_K_OTHER = 0, 1, 2, 3
 
 # every symbol include/dv.h declares
@@ -25,7 +26,9 @@ EXPORTS = ("dv_verify_init", "dv_verify_step", "dv_verify_step_sampled", "dv_acc
            "dv_accept_sampled_noalloc",
            "dv_draft_init", "dv_draft_forward", "dv_draft_tree",
            "dv_kv_commit", "dv_prefill", "dv_verify_free", "dv_last_error", "dv_tree_prepare",
-           "dv_profile_enable", "dv_profile_read")
+           "dv_profile_enable", "dv_profile_read",
+           "dv_kvq_store", "dv_kvq_load", "dv_kvq_advance", "dv_kvq_attention", "dv_kvq_attention_workspace",
+           "dv_verify_step_kvq", "dv_verify_step_kvq_sampled", "dv_prefill_kvq", "dv_kvq_commit")
 
 
 class DvError(RuntimeError):
@@ -61,6 +64,13 @@ class dv_dgf_weights(ctypes.Structure):
 
 class dv_kv(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("capacity", ctypes.c_int32), ("len", ctypes.c_int32)]
+
+
+class dv_kvq(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("scale", ctypes.c_void_p),
+                ("k_tail", ctypes.c_void_p), ("v_tail", ctypes.c_void_p), ("n_layers", ctypes.c_int32),
+                ("n_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("format", ctypes.c_int32),
                 ("capacity", ctypes.c_int32), ("len", ctypes.c_int32)]
 
 
@@ -127,6 +137,25 @@ def lib():
         L.dv_profile_read.argtypes = [vp, i32, ctypes.POINTER(ctypes.c_double),
                                       ctypes.POINTER(ctypes.c_int64), i32]
         L.dv_profile_read.restype = ctypes.c_int
+        i64, kvqp, accp = ctypes.c_int64, ctypes.POINTER(dv_kvq), ctypes.POINTER(dv_accept)
+        L.dv_kvq_store.argtypes = [kvqp, ctypes.POINTER(dv_kv), i32, vp]
+        L.dv_kvq_store.restype = ctypes.c_int
+        L.dv_kvq_load.argtypes = [kvqp, ctypes.POINTER(dv_kv), vp]
+        L.dv_kvq_load.restype = ctypes.c_int
+        L.dv_kvq_advance.argtypes = [kvqp, i32p, i32, vp]
+        L.dv_kvq_advance.restype = ctypes.c_int
+        L.dv_kvq_attention.argtypes = [kvqp, i32, vp, i64, i32, i32, vp, vp, i64, vp, i64, vp]
+        L.dv_kvq_attention.restype = ctypes.c_int
+        L.dv_kvq_attention_workspace.argtypes = [kvqp, i32, i32]
+        L.dv_kvq_attention_workspace.restype = i64
+        L.dv_verify_step_kvq.argtypes = [vp, i32p, i32p, i32, kvqp, vp, accp]
+        L.dv_verify_step_kvq.restype = ctypes.c_int
+        L.dv_verify_step_kvq_sampled.argtypes = [vp, i32p, i32p, i32, kvqp, vp, ctypes.c_float, f32p, f32p, vp, accp]
+        L.dv_verify_step_kvq_sampled.restype = ctypes.c_int
+        L.dv_prefill_kvq.argtypes = [vp, i32p, i32, kvqp, i32p]
+        L.dv_prefill_kvq.restype = ctypes.c_int
+        L.dv_kvq_commit.argtypes = [vp, kvqp, accp]
+        L.dv_kvq_commit.restype = ctypes.c_int
         _lib = L
     return _lib
 
@@ -257,6 +286,74 @@ def dv_prefill(h, tokens, kv: dv_kv) -> int:
     nxt = ctypes.c_int32(-1)
     _check(lib().dv_prefill(h, _ptr(t), len(t), ctypes.byref(kv), ctypes.byref(nxt)), h)
     return int(nxt.value)
+
+
+def dv_kvq_store(kvq: dv_kvq, kv: dv_kv, n: int, stream: int = 0):
+    """Append rows [kvq.len, kvq.len + n) of the bf16 cache kv."""
+    _check(lib().dv_kvq_store(kvq, kv, n, stream or None), None)
+
+
+def dv_kvq_load(kvq: dv_kvq, kv: dv_kv, stream: int = 0):
+    """Read the committed rows back into the bf16 cache kv."""
+    _check(lib().dv_kvq_load(kvq, kv, stream or None), None)
+
+
+def dv_kvq_advance(kvq: dv_kvq, path, stream: int = 0):
+    """path: host array of new rows, increasing."""
+    p = _i32(path)
+    _check(lib().dv_kvq_advance(kvq, _ptr(p), len(p), stream or None), None)
+
+
+def dv_kvq_attention_workspace(kvq: dv_kvq, n: int, n_heads: int) -> int:
+    """Bytes of workspace that dv_kvq_attention needs for n rows of n_heads."""
+    size = int(lib().dv_kvq_attention_workspace(kvq, n, n_heads))
+    if size < 0:
+        _check(size, None)
+    return size
+
+
+def dv_kvq_attention(kvq: dv_kvq, layer: int, q: int, q_stride: int, n: int, n_heads: int, mask, out: int,
+                     out_stride: int, workspace: int = 0, workspace_bytes: int = 0, stream: int = 0):
+    """q / out / workspace: device addresses, strides in floats; mask: host array of
+    n uint64, or None (row i sees new rows 0..i)."""
+    m = None
+    if mask is not None:
+        m = np.ascontiguousarray(mask, dtype=np.uint64)
+        if len(m) < n:
+            raise ValueError("mask needs one entry per row")
+    _check(lib().dv_kvq_attention(kvq, layer, q or None, q_stride, n, n_heads, None if m is None else m.ctypes.data,
+                                  out or None, out_stride, workspace or None, workspace_bytes, stream or None), None)
+
+
+def dv_verify_step_kvq(h, tokens, tree_parents, kvq: dv_kvq, out_logits: int = 0) -> dv_accept:
+    t, p = _i32(tokens), _i32(tree_parents)
+    acc = dv_accept()
+    _check(lib().dv_verify_step_kvq(h, _ptr(t), _ptr(p), len(t), kvq, out_logits or None, acc), h)
+    return acc
+
+
+def dv_verify_step_kvq_sampled(h, tokens, tree_parents, kvq: dv_kvq, draft_probs: int, temperature: float, u_accept,
+                               u_bonus, out_logits: int = 0) -> dv_accept:
+    """draft_probs / out_logits: device addresses; u_accept / u_bonus: host arrays."""
+    t, p = _i32(tokens), _i32(tree_parents)
+    ua, ub = _f32(u_accept), _f32(u_bonus)
+    if len(ua) < len(t) or len(ub) < len(t):
+        raise ValueError("u_accept and u_bonus need one entry per tree node")
+    acc = dv_accept()
+    _check(lib().dv_verify_step_kvq_sampled(h, _ptr(t), _ptr(p), len(t), kvq, draft_probs or None, float(temperature),
+                                            _fptr(ua), _fptr(ub), out_logits or None, acc), h)
+    return acc
+
+
+def dv_prefill_kvq(h, tokens, kvq: dv_kvq) -> int:
+    t = _i32(tokens)
+    nxt = ctypes.c_int32(-1)
+    _check(lib().dv_prefill_kvq(h, _ptr(t), len(t), kvq, nxt), h)
+    return int(nxt.value)
+
+
+def dv_kvq_commit(h, kvq: dv_kvq, accept: dv_accept):
+    _check(lib().dv_kvq_commit(h, kvq, accept), h)
 
 
 def dv_verify_free(h):
