@@ -3,6 +3,8 @@
 #include <hip/hip_runtime_api.h>
 
 #include <algorithm>
+#include <atomic>
+#include <chrono>
 #include <cstring>
 #include <mutex>
 
@@ -103,14 +105,25 @@ KvqAttnArgs attention_args(const dv_kvq *c, int layer, int n)
     return a;
 }
 
-void set_cut(KvqAttnArgs &a, const KvqCut &cut, int hd, float *ws)
+// A number that no other call of this process has, from a start that no memory holds
+// by chance; 48 bits, above a count's 16.
+uint64_t next_tag()
+{
+    static std::atomic<uint64_t> count{(uint64_t)std::chrono::steady_clock::now().time_since_epoch().count() * 0x9e3779b97f4a7c15ull >> 16};
+    return (count.fetch_add(1, std::memory_order_relaxed) | 1ull << 47) << 16;
+}
+
+// The cut, and its parts of the workspace.
+void set_cut(KvqAttnArgs &a, const KvqCut &cut, int hd, void *ws)
 {
     const size_t rows = (size_t)a.H * cut.n_split * a.n * a.G;
     a.per_split = cut.per_split;
     a.n_split = cut.n_split;
-    a.part_o = ws;
-    a.part_m = ws + rows * hd;
-    a.part_l = a.part_m + rows;
+    if (cut.n_split == 1) return;
+    a.arrived = static_cast<uint64_t *>(ws);
+    a.part_o = reinterpret_cast<float *>(static_cast<char *>(ws) + kvq_words_bytes(a.H, cut.z));
+    a.part_ml = reinterpret_cast<uint64_t *>(a.part_o + rows * hd);
+    a.tag = next_tag();
 }
 
 // The handle's step and prompts over an 8-bit cache: a step's nodes go to the tail
@@ -139,16 +152,9 @@ struct KvqSeam final : CacheSeam {
         a.half = s.tm.half;
         a.rows_out = s.out_split ? (s.tm.half ? 8 : s.tm.Mpad) : a.n;
         std::memcpy(a.mask, s.tm.anc, sizeof a.mask);
-        KvqCut cut = kvq_cut(a.H, a.n, a.tiles, h->n_cu);
-        if (cut.n_split > h->attn_split_max) {  // what the handle's partials hold
-            cut.per_split = (a.tiles + h->attn_split_max - 1) / h->attn_split_max;
-            cut.n_split = (a.tiles + cut.per_split - 1) / cut.per_split;
-        }
-        a.per_split = cut.per_split;
-        a.n_split = cut.n_split;
-        a.part_o = h->part_o;
-        a.part_m = h->part_m;
-        a.part_l = h->part_l;
+        // (the handle's partials hold 512 workgroups' sums of 64 rows)
+        const KvqCut cut = kvq_cut(a.H, a.n, a.tiles, std::min(h->n_cu, 256));
+        set_cut(a, cut, s.hd, h->part_o);
         return launch_kvq_attention(a, s.hd, c->format == DV_F8, cut, h->stream);
     }
     hipError_t committed(int n) override
@@ -258,8 +264,8 @@ int64_t dv_kvq_attention_workspace(const dv_kvq *c, int32_t n, int32_t n_heads)
     const hipError_t e = current_cus(&n_cu);
     if (e != hipSuccess) return set_err(nullptr, DV_EHIP, "compute units: %s", hipGetErrorString(e));
     const int rows = n * (n_heads / c->n_heads), tiles = c->capacity / KVQ_BLOCK + KVQ_TAIL / KVQ_BLOCK;
-    return (int64_t)kvq_attention_floats(c->n_heads, rows, c->head_dim,
-                                         std::min(kvq_max_split(c->n_heads, rows, n_cu), tiles)) * 4;
+    return (int64_t)kvq_attention_bytes(c->n_heads, rows, c->head_dim,
+                                        std::min(kvq_max_split(c->n_heads, rows, n_cu), tiles));
 }
 
 int dv_kvq_attention(const dv_kvq *c, int32_t layer, const float *q, int64_t q_stride, int32_t n, int32_t n_heads,
@@ -291,10 +297,10 @@ int dv_kvq_attention(const dv_kvq *c, int32_t layer, const float *q, int64_t q_s
     a.ldo = out_stride;
     for (int i = 0; i < n; ++i) a.mask[i] = mask ? mask[i] : ~0ull >> (63 - i);
     const KvqCut cut = kvq_cut(a.H, n * a.G, a.tiles, n_cu);
-    const size_t need = kvq_attention_floats(a.H, n * a.G, c->head_dim, cut.n_split) * 4;
+    const size_t need = kvq_attention_bytes(a.H, n * a.G, c->head_dim, cut.n_split);
     if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < 0 || (size_t)workspace_bytes < need))
         return set_err(nullptr, DV_EINVAL, "attention needs a 16-byte aligned workspace of %zu bytes", need);
-    set_cut(a, cut, c->head_dim, static_cast<float *>(workspace));
+    set_cut(a, cut, c->head_dim, workspace);
     e = launch_kvq_attention(a, c->head_dim, c->format == DV_F8, cut, static_cast<hipStream_t>(stream));
     if (e != hipSuccess) return set_err(nullptr, DV_EHIP, "cache attention launch: %s", hipGetErrorString(e));
     return DV_OK;

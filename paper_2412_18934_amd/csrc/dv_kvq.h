@@ -10,6 +10,8 @@
 #define KVQ_BLOCK 32      // slots that share a scale
 #define KVQ_TAIL 96       // bf16 slots per head behind the last whole block: 31 committed + 64 new
 #define KVQ_MAX_NEW 64    // new rows of one call
+#define KVQ_MAX_SPLIT 256 // ranges of a head's keys
+#define KVQ_WORD 16       // 8-byte words from one counter to the next: counters of one line queue up
 
 // Consecutive layers of a cache (L of them, from the pointers' layer on).
 struct KvqLayers {
@@ -40,13 +42,13 @@ hipError_t launch_kvq_advance(const KvqLayers &c, const int32_t *path, int n, hi
 struct KvqCut {
     int rt, z, per_split, n_split;
 };
-inline int kvq_row_tiles(int rows) { return rows <= 16 ? 1 : rows <= 32 ? 2 : 4; }
+inline int kvq_row_tiles(int rows) { return rows <= 16 ? 1 : 2; }
 inline int kvq_row_groups(int rows) { return (rows + 16 * kvq_row_tiles(rows) - 1) / (16 * kvq_row_tiles(rows)); }
 // the most ranges of any cache length: about one workgroup per CU
 inline int kvq_max_split(int heads, int rows, int n_cu)
 {
     const int most = n_cu / (heads * kvq_row_groups(rows));
-    return most > 1 ? most : 1;
+    return most < 1 ? 1 : most > KVQ_MAX_SPLIT ? KVQ_MAX_SPLIT : most;
 }
 inline KvqCut kvq_cut(int heads, int rows, int tiles, int n_cu)
 {
@@ -55,13 +57,17 @@ inline KvqCut kvq_cut(int heads, int rows, int tiles, int n_cu)
     c.z = kvq_row_groups(rows);
     const int most = kvq_max_split(heads, rows, n_cu);
     c.per_split = (tiles + most - 1) / most;
+    if (c.per_split < 8) c.per_split = 8;  // a tile for each wave
     c.n_split = (tiles + c.per_split - 1) / c.per_split;
     return c;
 }
-// floats of workspace of n_split ranges (one writes the output itself)
-inline size_t kvq_attention_floats(int heads, int rows, int hd, int n_split)
+// Workspace of n_split ranges (one writes the output itself): a word of arrivals for
+// each head and row group, then the partial sums, references and weights.
+inline size_t kvq_words_bytes(int heads, int z) { return (size_t)heads * z * KVQ_WORD * 8; }
+inline size_t kvq_attention_bytes(int heads, int rows, int hd, int n_split)
 {
-    return n_split == 1 ? 0 : (size_t)heads * n_split * rows * (hd + 2);
+    if (n_split == 1) return 0;
+    return kvq_words_bytes(heads, kvq_row_groups(rows)) + (size_t)heads * n_split * rows * (hd + 2) * 4;
 }
 
 struct KvqAttnArgs {
@@ -80,7 +86,10 @@ struct KvqAttnArgs {
     int32_t Mpad, half;
     int32_t rows_out;            // rows to write: n G, or with out_split its padding too (zeros)
     int32_t tiles, per_split, n_split;
-    float *part_o, *part_m, *part_l;  // [H][n_split][rows][hd] unnormalised, [H][n_split][rows]
+    float *part_o;               // [H][n_split][rows][hd] unnormalised sums
+    uint64_t *part_ml;           // [H][n_split][rows]: reference and sum of weights
+    uint64_t *arrived;           // [H][row groups]
+    uint64_t tag;                // this call's, in the upper 48 bits
     uint64_t mask[KVQ_MAX_NEW];  // bit j: new row i sees new row j
 };
 hipError_t launch_kvq_attention(const KvqAttnArgs &a, int hd, int f8, const KvqCut &cut, hipStream_t s);

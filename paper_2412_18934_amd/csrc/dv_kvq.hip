@@ -9,6 +9,8 @@
 //      8 (n / 4) + 4 t + n % 4, dims 64 p + 8 g .. +8, then 64 p + 32 + 8 g .. +8;
 //   V: for each 32 dims p, 1 KB: lane l holds slots 8 g .. +8 of dim 32 p + n, then
 //      of dim 32 p + 16 + n.
+#include <type_traits>
+
 #include "dv_device.h"
 #include "dv_internal.h"
 #include "dv_kvq.h"
@@ -349,20 +351,62 @@ template <bool F8, int HD> __global__ __launch_bounds__(256) void k_kvq_advance(
 //   ones, and new row j where bit j of its mask is set;
 //   o_i = sum_j exp(s_ij - m_i) v_j / sum_j exp(s_ij - m_i), 0 if it sees none.
 //
-// Workgroup (split, KV head, row tile): its 4 waves take interleaved 32-key tiles
-// of the range (blocks of codes, then up to three tiles of the tail) with a
-// running maximum and sum per query row, and are combined in LDS; a second launch
-// combines the ranges.  Rows are the n new tokens x the G query heads that share
-// the KV head.  Scores are in base-2 units.
+// Workgroup (split, KV head, row group): its waves take interleaved 32-key tiles of
+// the range (blocks of codes, then up to three tiles of the tail) with a running
+// reference m and sum per query row, and are combined in LDS; the last range of a
+// head and row group to finish combines the ranges, in their order.  Rows are the n
+// new tokens x the G query heads that share the KV head.
 //
-//   S^T = K Q^T: A = 16 keys x 32 dims; D gives lane (n, g) the scores of row n for
-//   the 8 consecutive keys 8 g .. +8 of the tile; O = P V takes those as A.
-// Codes are exact in bf16, so K and V go into the matrix instructions as codes and
-// their scales onto the scores and the weights, in fp32.  Queries and weights
-// are fp32 numbers, each cut into three bf16 (8 + 8 + 8 bits, nothing lost).
+//   S^T = K Q^T: A = 16 keys x dims, B = queries; D gives lane (n, g) the scores of
+//   row n for the 8 consecutive keys 8 g .. +8 of the tile, which are the B operand
+//   of O^T = V^T P^T; its D has 4 consecutive dims of row n.  So a row's numbers all
+//   belong to lanes n + 16 g, and only its reference ever crosses lanes.
+//
+// Codes enter the matrix instructions as codes, scales go onto scores and weights.
+// Each query and weight is one fp32 number in parts:
+//   int8 K: q as a 23-bit integer relative to its row's largest, in three signed bytes;
+//     the products are exact integers, and K's bytes are operands as they stand;
+//   e4m3 K: q in two fp16 (11 + 11 bits), its row scaled to a largest of 2^10 .. 2^11
+//     so that the low part stays normal; e4m3 is exact in fp16;
+//   V: weights in two fp16; int8 and e4m3 are exact in fp16;
+//   tail: bf16, whose range fp16 has not; q and weights in three bf16 (8 + 8 + 8).
+// Weights are exp2(s - m) with m a reference that a row's scores exceed by at most
+// LAZY (in base 2): it moves, and the sums are rescaled, only when a score is further
+// above it, which after the first tiles is rare.  V's scales likewise: the sums are
+// in units of the largest scale so far.  So a weight is at most 2^(LAZY + 11) = 2^15 in
+// fp16, which holds 65504.
 
-// fp32 -> three bf16 by truncation: their sum is the number (unless it is near the
-// smallest ones)
+constexpr float LAZY = 4.f, W_UNIT = 2048.f;
+
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ uint32_t bits_of(f16x2 x) { return __builtin_bit_cast(uint32_t, x); }
+
+// Eight codes as fp16.  int8: 0x6400 + (code + 128) is 1024 + 128 + code.
+template <bool F8> __device__ __forceinline__ u32x4 f16_of(uint32_t lo, uint32_t hi)
+{
+    u32x4 r;
+    if constexpr (F8) {
+        r[0] = bits_of((f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false));
+        r[1] = bits_of((f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true));
+        r[2] = bits_of((f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false));
+        r[3] = bits_of((f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true));
+    } else {
+        const f16x2 off = {(_Float16)-1152.f, (_Float16)-1152.f};
+        const uint32_t w[2] = {lo ^ 0x80808080u, hi ^ 0x80808080u};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t x = __builtin_amdgcn_perm(0x64646464u, w[i >> 1], i & 1 ? 0x07030702u : 0x07010700u);
+            r[i] = bits_of(__builtin_bit_cast(f16x2, x) + off);
+        }
+    }
+    return r;
+}
+
+// Eight fp32 numbers as three bf16 each, by truncation: their sum is the number
+// (unless it is near the smallest ones).
 __device__ __forceinline__ void split3(const float *v, u32x4 (&t)[3])
 {
 #pragma unroll
@@ -382,18 +426,31 @@ __device__ __forceinline__ void split3(const float *v, u32x4 (&t)[3])
     }
 }
 
-__device__ __forceinline__ f32x4 mfma(const u32x4 &a, const u32x4 &b, const f32x4 &c)
+// Eight fp32 numbers of at most 65504 as two fp16 each, by truncation: 2^-22 of the
+// number, or 2^-24, is lost at most.
+__device__ __forceinline__ void split2(const float *v, u32x4 (&t)[2])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const f16x2 h = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(v[2 * i], v[2 * i + 1]));
+        t[0][i] = bits_of(h);
+        t[1][i] = bits_of(__builtin_bit_cast(
+            f16x2, __builtin_amdgcn_cvt_pkrtz(v[2 * i] - (float)h[0], v[2 * i + 1] - (float)h[1])));
+    }
+}
+
+__device__ __forceinline__ f32x4 mfma_bf16(const u32x4 &a, const u32x4 &b, const f32x4 &c)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
-
-// What a tile is made of.
-struct Codes {
-    static constexpr bool value = false;
-};
-struct Tail {
-    static constexpr bool value = true;
-};
+__device__ __forceinline__ f32x4 mfma_f16(const u32x4 &a, const u32x4 &b, const f32x4 &c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ i32x4 mfma_i8(const u32x4 &a, const u32x4 &b, const i32x4 &c)
+{
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i32x4, a), __builtin_bit_cast(i32x4, b), c, 0, 0, 0);
+}
 
 // Row `row` of KV head h is query head h G + row % G of token row / G.
 __device__ __forceinline__ void write_out(const KvqAttnArgs &a, int hd, int h, int row, int d0, const float (&o)[4])
@@ -405,273 +462,465 @@ __device__ __forceinline__ void write_out(const KvqAttnArgs &a, int hd, int h, i
         *reinterpret_cast<float4 *>(a.out + i * a.ldo + col) = make_float4(o[0], o[1], o[2], o[3]);
 }
 
-template <int HD, bool F8, int RT> __global__ __launch_bounds__(256) void k_kvq_attn(KvqAttnArgs a)
+// Whether this is the last of n workgroups to get here, each once.  The word may
+// start as anything: it counts under the call's tag (48 bits, the count below them).
+// A workgroup that does not find the tag sets it, with itself as the first, or finds
+// it set by another one and is counted then; one that finds it has been counted.
+__device__ __forceinline__ bool last_of(uint64_t *w, uint64_t tag, int n)
 {
-    constexpr int NW = 4, NC = HD / 32, ND = HD / 16;
-    const int split = blockIdx.x, h = blockIdx.y, row0 = blockIdx.z * 16 * RT;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n = lane & 15, g = lane >> 4;
-    const int rows = a.n * a.G;
-    const float scale2 = 1.4426950408889634f / sqrtf((float)HD);
-    __shared__ u32x4 sm_q[RT][NC * 3 * 64];
-    __shared__ float sm_m[NW][16], sm_l[NW][16];
-    __shared__ __align__(16) float sm_o[NW][16][HD + 4];
+    uint64_t old = __hip_atomic_fetch_add(w, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    while (old >> 16 != tag >> 16) {
+        uint64_t cur = __hip_atomic_load(w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        if (cur >> 16 == tag >> 16)
+            old = __hip_atomic_fetch_add(w, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        else if (__hip_atomic_compare_exchange_strong(w, &cur, tag | 1, __ATOMIC_RELAXED, __ATOMIC_RELAXED,
+                                                      __HIP_MEMORY_SCOPE_AGENT))
+            old = tag;
+    }
+    return (int)(old & 0xffff) == n - 1;
+}
 
-    // queries into LDS as B operands: 8 dims of one row per thread and pass
-    for (int e = threadIdx.x; e < RT * 16 * (HD / 8); e += 256) {
-        const int d8 = e % (HD / 8), row = e / (HD / 8), c = d8 >> 2, qg = d8 & 3;
-        float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        if (row0 + row < rows) {
-            const float *p = a.q + ((row0 + row) / a.G) * a.ldq + (h * a.G + (row0 + row) % a.G) * HD + d8 * 8;
-            const float4 x = *reinterpret_cast<const float4 *>(p), y = *reinterpret_cast<const float4 *>(p + 4);
-            v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w, v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
-        }
-        u32x4 t[3];
-        split3(v, t);
+// f(0), .. f(N - 1) with constant arguments: a row tile's registers are never indexed
+template <int N, typename F> __device__ __forceinline__ void each(F f)
+{
+    if constexpr (N > 0) {
+        each<N - 1>(f);
+        f(std::integral_constant<int, N - 1>{});
+    }
+}
+
+template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW) void k_kvq_attn(KvqAttnArgs a)
+{
+    constexpr int NC = HD / 32, ND = HD / 16;
+    constexpr int NQ = F8 ? 2 * NC : 3 * (HD / 64);  // KB of a row tile's query parts for codes
+    constexpr int NT = 3 * NC;                       // and for the tail
+    const int split = blockIdx.x, h = blockIdx.y, row0 = blockIdx.z * 16 * RT;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
+    const int rows = a.n * a.G;
+    constexpr float scale2 = HD == 128 ? 1.4426950408889634f / 11.313708498984761f : 1.4426950408889634f / 8.f;
+
+    // query parts as operands; later the waves' sums
+    constexpr int SUMS = NW * 16 * (HD + 4) * 4, PARTS = RT * (NQ + NT) * 1024;
+    __shared__ __align__(16) char sm[SUMS > PARTS ? SUMS : PARTS];
+    __shared__ float sm_m[NW][16], sm_l[NW][16], sm_c[16 * RT];
+    u32x4(*qc)[NQ * 64] = reinterpret_cast<u32x4(*)[NQ * 64]>(sm);
+    u32x4(*qt)[NT * 64] = reinterpret_cast<u32x4(*)[NT * 64]>(sm + RT * NQ * 1024);
+    float(*sm_o)[16][HD + 4] = reinterpret_cast<float(*)[16][HD + 4]>(sm);
+
+    struct Raw {
+        u32x4 k[NC], v[NC];
+        float2 s;
+    };
+    auto load = [&](int t, Raw &x) {
+        const int64_t at = (int64_t)h * a.nb + t;
+        const uint8_t *kp = a.k + at * KVQ_BLOCK * HD + lane * 16, *vp = a.v + at * KVQ_BLOCK * HD + lane * 16;
+        x.s = *reinterpret_cast<const float2 *>(a.scale + at * 2);
 #pragma unroll
-        for (int p = 0; p < 3; ++p) sm_q[row / 16][(c * 3 + p) * 64 + 16 * qg + row % 16] = t[p];
+        for (int j = 0; j < NC; ++j) x.k[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(kp + j * 1024));
+#pragma unroll
+        for (int j = 0; j < NC; ++j) x.v[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(vp + j * 1024));
+    };
+    const int t0 = split * a.per_split, t1 = min(a.tiles, t0 + a.per_split), c1 = min(t1, a.blocks);
+    const bool has_tail = t1 > a.blocks;
+    Raw buf0, buf1;
+
+    // 8 dims of one row per thread; a row's threads are neighbours.  (Loads return in
+    // order: the queries' go ahead of the first tile's.)
+    static_assert(RT * 16 * (HD / 8) <= 64 * NW, "a thread per 8 query numbers");
+    const int d8 = tid % (HD / 8), qrow = tid / (HD / 8);
+    float4 qx = make_float4(0.f, 0.f, 0.f, 0.f), qy = qx;
+    if (qrow < RT * 16 && row0 + qrow < rows) {
+        const float *p = a.q + ((row0 + qrow) / a.G) * a.ldq + (h * a.G + (row0 + qrow) % a.G) * HD + d8 * 8;
+        qx = *reinterpret_cast<const float4 *>(p);
+        qy = *reinterpret_cast<const float4 *>(p + 4);
+    }
+    if (t0 + wave < c1) load(t0 + wave, buf0);
+    if (qrow < RT * 16) {
+        const int row = qrow, c = d8 >> 2, at = 16 * (d8 & 3) + row % 16;
+        const float v[8] = {qx.x, qx.y, qx.z, qx.w, qy.x, qy.y, qy.z, qy.w};
+        // the row's largest, as bits (NaN is above infinity)
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
+#pragma unroll
+        for (int off = 1; off < HD / 8; off <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off));
+        // 2^ex is at most the largest; below 2^-100 a row counts as 0
+        const int ex = max((int)(top >> 23) - 127, -100), to = F8 ? 10 : 21;
+        const float f = __uint_as_float((uint32_t)(127 + to - ex) << 23);  // (ex 128: 2^-118 or 2^-107)
+        if (d8 == 0) sm_c[row] = top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : scale2 * __uint_as_float((uint32_t)(127 - to + ex) << 23);
+        if constexpr (F8) {
+            float y[8];
+            u32x4 t[2];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = v[i] * f;
+            split2(y, t);
+            qc[row / 16][(2 * c) * 64 + at] = t[0];
+            qc[row / 16][(2 * c + 1) * 64 + at] = t[1];
+        } else {
+            uint32_t d[3][2] = {};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                int y = (int)rintf(v[i] * f);  // at most 2^22
+#pragma unroll
+                for (int p = 0; p < 3; ++p) {
+                    const int low = (int)(int8_t)y;
+                    d[p][i >> 2] |= (uint32_t)(low & 0xff) << (8 * (i & 3));
+                    y = (y - low) >> 8;
+                }
+            }
+#pragma unroll
+            for (int p = 0; p < 3; ++p)
+                reinterpret_cast<uint2 *>(&qc[row / 16][(p * (HD / 64) + (c >> 1)) * 64 + at])[c & 1] = make_uint2(d[p][0], d[p][1]);
+        }
+        if (has_tail) {
+            u32x4 t[3];
+            split3(v, t);
+#pragma unroll
+            for (int p = 0; p < 3; ++p) qt[row / 16][(c * 3 + p) * 64 + at] = t[p];
+        }
     }
     uint64_t mask[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         const int row = row0 + 16 * rt + n;
-        mask[rt] = row < rows ? a.mask[row / a.G] : 0ull;
+        mask[rt] = has_tail && row < rows ? a.mask[row / a.G] : 0ull;
     }
     __syncthreads();
 
-    float m_run[RT], l_run[RT];
+    float m_run[RT], l_run[RT], coef[RT];  // (l_run: of the lane's own keys)
     f32x4 o[RT][ND];
+    float v_unit = 0.f, v_inv = 0.f;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         m_run[rt] = -INFINITY;
         l_run[rt] = 0.f;
+        coef[rt] = sm_c[16 * rt + n];
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) o[rt][dt] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
 
-    // one tile of 32 keys as bf16 operands.  From the tail (slots from tail0 on): `left`
-    // of them exist, and new rows are seen by the rows whose mask says so; `odd`: the
-    // tile of V where numbers are infinite or NaN (taken out of the operand), or null.
-    auto process = [&](auto from_tail, const u32x4 (&ka)[NC], const u32x4 (&kb)[NC], const u32x4 (&v)[ND], float ks, float vs,
-                       int tail0, int left, const uint16_t *odd) {
-        constexpr bool tail = decltype(from_tail)::value;
+    // moves row tile rt's reference to at least mt (one lane's maximum of the row)
+    auto move = [&](auto rt_, float mt) {
+        constexpr int rt = decltype(rt_)::value;
+        mt = fmaxf(mt, __shfl_xor(mt, 16));
+        mt = fmaxf(mt, __shfl_xor(mt, 32));
+        const float mnew = fmaxf(m_run[rt], mt);
+        const float alpha = m_run[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run[rt] - mnew);
+        l_run[rt] *= alpha;
 #pragma unroll
-        for (int rt = 0; rt < RT; ++rt) {
-            if (row0 + 16 * rt >= rows) break;
-            f32x4 sa = (f32x4){0.f, 0.f, 0.f, 0.f}, sb = sa;
+        for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-            for (int c = 0; c < NC; ++c)
-#pragma unroll
-                for (int p = 0; p < 3; ++p) {
-                    const u32x4 q = sm_q[rt][(c * 3 + p) * 64 + lane];
-                    sa = mfma(ka[c], q, sa);
-                    sb = mfma(kb[c], q, sb);
-                }
-            float sv[8], mt = -INFINITY;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                sv[i] = (i < 4 ? sa[i] : sb[i - 4]) * (ks * scale2);
-                if constexpr (tail) {
-                    const int j = tail0 + 8 * g + i - a.r;  // new row of the key, or committed
-                    if (8 * g + i >= left || (j >= 0 && !((mask[rt] >> (j & 63)) & 1ull))) sv[i] = -INFINITY;
-                }
-                mt = fmaxf(mt, sv[i]);
-            }
-            mt = fmaxf(mt, __shfl_xor(mt, 16));
-            mt = fmaxf(mt, __shfl_xor(mt, 32));
-            const float mnew = fmaxf(m_run[rt], mt);
-            const float alpha = m_run[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m_run[rt] - mnew);
-            float ps = 0.f, pv[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                pv[i] = sv[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sv[i] - mnew);
-                ps += pv[i];
-                pv[i] *= vs;
-            }
-            ps += __shfl_xor(ps, 16);
-            ps += __shfl_xor(ps, 32);
-            l_run[rt] = l_run[rt] * alpha + ps;
-            m_run[rt] = mnew;
-            float al[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) al[j] = __shfl(alpha, 4 * g + j);
-            u32x4 p3[3];
-            split3(pv, p3);
-#pragma unroll
-            for (int dt = 0; dt < ND; ++dt) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) o[rt][dt][j] *= al[j];
-#pragma unroll
-                for (int p = 0; p < 3; ++p) o[rt][dt] = mfma(p3[p], v[dt], o[rt][dt]);
-            }
-            if constexpr (tail) {
-                if (!odd) continue;
-                // such a number counts for the rows that see its key, and is nothing (not
-                // 0 x infinity) for the others
-                for (int kg = 0; kg < 4; ++kg)
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        if (8 * kg + i >= left) break;
-                        float pr[4];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) pr[j] = __shfl(pv[i], 16 * kg + 4 * g + j);
-#pragma unroll
-                        for (int dt = 0; dt < ND; ++dt) {
-                            const float x = bf2f(odd[(dt * 16 + n) * 32 + 8 * kg + i]);
-                            if (__builtin_isfinite(x)) continue;
-#pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                if (pr[j] != 0.f) o[rt][dt][j] += pr[j] * x;
-                        }
-                    }
-            }
-        }
+            for (int j = 0; j < 4; ++j) o[rt][dt][j] *= alpha;
+        m_run[rt] = mnew;
     };
 
-    const int t0 = split * a.per_split, t1 = min(a.tiles, t0 + a.per_split);
-    const int c1 = min(t1, a.blocks);
-    u32x4 ka[NC], kb[NC], v[ND];
-    for (int t = t0 + wave; t < c1; t += NW) {
-        const int64_t at = (int64_t)h * a.nb + t;
-        const uint8_t *kp = a.k + at * KVQ_BLOCK * HD + lane * 16, *vp = a.v + at * KVQ_BLOCK * HD + lane * 16;
-        const float2 sc = *reinterpret_cast<const float2 *>(a.scale + at * 2);
-        u32x4 kr[NC], vr[NC];
+    auto codes = [&](const Raw &x) {
+        if (x.s.y > v_unit) {
+            const float r = v_unit / x.s.y;
 #pragma unroll
-        for (int j = 0; j < NC; ++j) {
-            kr[j] = *reinterpret_cast<const u32x4 *>(kp + j * 1024);
-            vr[j] = *reinterpret_cast<const u32x4 *>(vp + j * 1024);
+            for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) o[rt][dt][j] *= r;
+            v_unit = x.s.y;
+            v_inv = 1.f / x.s.y;
         }
-#pragma unroll
-        for (int j = 0; j < NC / 2; ++j)
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                ka[2 * j + half] = bf16_of<F8>(kr[2 * j][2 * half], kr[2 * j][2 * half + 1]);
-                kb[2 * j + half] = bf16_of<F8>(kr[2 * j + 1][2 * half], kr[2 * j + 1][2 * half + 1]);
-            }
+        const float vs = x.s.y * v_inv * W_UNIT;
+        u32x4 v[ND];
 #pragma unroll
         for (int j = 0; j < NC; ++j)
 #pragma unroll
-            for (int half = 0; half < 2; ++half) v[2 * j + half] = bf16_of<F8>(vr[j][2 * half], vr[j][2 * half + 1]);
-        process(Codes{}, ka, kb, v, sc.x, sc.y, 0, KVQ_BLOCK, nullptr);
+            for (int half = 0; half < 2; ++half) v[2 * j + half] = f16_of<F8>(x.v[j][2 * half], x.v[j][2 * half + 1]);
+        u32x4 ka[NC], kb[NC];  // e4m3 as fp16
+        if constexpr (F8)
+#pragma unroll
+            for (int j = 0; j < NC / 2; ++j)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    ka[2 * j + half] = f16_of<true>(x.k[2 * j][2 * half], x.k[2 * j][2 * half + 1]);
+                    kb[2 * j + half] = f16_of<true>(x.k[2 * j + 1][2 * half], x.k[2 * j + 1][2 * half + 1]);
+                }
+        each<RT>([&](auto rt_) {
+            constexpr int rt = decltype(rt_)::value;
+            if (row0 + 16 * rt >= rows) return;
+            float s[8];
+            if constexpr (F8) {
+                f32x4 sa = (f32x4){0.f, 0.f, 0.f, 0.f}, sb = sa;
+#pragma unroll
+                for (int c = 0; c < 2 * NC; ++c) {
+                    const u32x4 q = qc[rt][c * 64 + lane];
+                    sa = mfma_f16(ka[c >> 1], q, sa);
+                    sb = mfma_f16(kb[c >> 1], q, sb);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[i] = sa[i], s[4 + i] = sb[i];
+            } else {
+                i32x4 sa[3] = {}, sb[3] = {};
+#pragma unroll
+                for (int c = 0; c < HD / 64; ++c)
+#pragma unroll
+                    for (int p = 0; p < 3; ++p) {
+                        const u32x4 q = qc[rt][(p * (HD / 64) + c) * 64 + lane];
+                        sa[p] = mfma_i8(x.k[2 * c], q, sa[p]);
+                        sb[p] = mfma_i8(x.k[2 * c + 1], q, sb[p]);
+                    }
+                // the low two digits' sums are below 2^30 together
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    s[i] = fmaf((float)sa[2][i], 65536.f, (float)(sa[1][i] * 256 + sa[0][i]));
+                    s[4 + i] = fmaf((float)sb[2][i], 65536.f, (float)(sb[1][i] * 256 + sb[0][i]));
+                }
+            }
+            const float c = coef[rt] * x.s.x;
+            float mt = s[0];
+#pragma unroll
+            for (int i = 1; i < 8; ++i) mt = fmaxf(mt, s[i]);
+            mt *= c;
+            if (__any(mt > m_run[rt] + LAZY)) move(rt_, mt);
+            float w[8], ps = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                w[i] = __builtin_amdgcn_exp2f(fmaf(s[i], c, -m_run[rt]));
+                ps += w[i];
+                w[i] *= vs;
+            }
+            l_run[rt] += ps;
+            u32x4 p2[2];
+            split2(w, p2);
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt) {
+                o[rt][dt] = mfma_f16(v[dt], p2[0], o[rt][dt]);
+                o[rt][dt] = mfma_f16(v[dt], p2[1], o[rt][dt]);
+            }
+        });
+    };
+    // two buffers in turn: the next tile loads while one is used
+    for (int t = t0 + wave; t < c1; t += 2 * NW) {
+        if (t + NW < c1) load(t + NW, buf1);
+        codes(buf0);
+        if (t + NW >= c1) break;
+        if (t + 2 * NW < c1) load(t + 2 * NW, buf0);
+        codes(buf1);
     }
-    // tail tiles of the range
-    for (int t = max(t0, a.blocks) + (wave + NW - (max(t0, a.blocks) - t0) % NW) % NW; t < t1; t += NW) {
+
+    // tail tiles of the range, by the waves whose turn it is
+    const int tt = max(t0, a.blocks);
+    for (int t = tt + (wave + NW - (tt - t0) % NW) % NW; t < t1; t += NW) {
         const int s0 = (t - a.blocks) * KVQ_BLOCK, left = min(KVQ_BLOCK, a.r + a.n - s0);
         const uint16_t *kp = a.kt + ((int64_t)h * KVQ_TAIL + s0) * HD + 8 * g;
-        const uint16_t *vp = a.vt + ((int64_t)h * KVQ_TAIL + s0) * HD + n * 32 + 8 * g;
+        const uint16_t *vt = a.vt + ((int64_t)h * KVQ_TAIL + s0) * HD;
+        u32x4 ka[NC], kb[NC], v[ND];
 #pragma unroll
         for (int c = 0; c < NC; ++c) {
             ka[c] = *reinterpret_cast<const u32x4 *>(kp + k_slot(lane, 0) * HD + 32 * c);
             kb[c] = *reinterpret_cast<const u32x4 *>(kp + k_slot(lane, 1) * HD + 32 * c);
         }
-        // slots past the last row hold anything
+        // V without the slots past the last row, which hold anything, and without its
+        // infinities and NaN, which come after
         bool odd = false;
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) {
-            v[dt] = *reinterpret_cast<const u32x4 *>(vp + dt * 512);
+            v[dt] = *reinterpret_cast<const u32x4 *>(vt + (dt * 16 + n) * 32 + 8 * g);
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                if (8 * g + 2 * w >= left) v[dt][w] = 0u;
-                else if (8 * g + 2 * w + 1 >= left) v[dt][w] &= 0xffffu;
-                const uint32_t x = v[dt][w];
+                uint32_t x = v[dt][w];
+                if (8 * g + 2 * w >= left) x = 0u;
+                else if (8 * g + 2 * w + 1 >= left) x &= 0xffffu;
                 const uint32_t is = ((x & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((x & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
                 v[dt][w] = x & ~is;
                 odd |= is != 0u;
             }
         }
-        process(Tail{}, ka, kb, v, 1.f, 1.f, s0, left, __any(odd) ? a.vt + ((int64_t)h * KVQ_TAIL + s0) * HD : nullptr);
+        odd = __any(odd);
+        if (v_unit == 0.f) v_unit = v_inv = 1.f;  // no sums yet, or only zeros
+        const float vs = v_inv * W_UNIT;
+        each<RT>([&](auto rt_) {
+            constexpr int rt = decltype(rt_)::value;
+            if (row0 + 16 * rt >= rows) return;
+            f32x4 sa = (f32x4){0.f, 0.f, 0.f, 0.f}, sb = sa;
+#pragma unroll
+            for (int c = 0; c < NT; ++c) {
+                const u32x4 q = qt[rt][c * 64 + lane];
+                sa = mfma_bf16(ka[c / 3], q, sa);
+                sb = mfma_bf16(kb[c / 3], q, sb);
+            }
+            float s[8], mt = -INFINITY;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                s[i] = (i < 4 ? sa[i] : sb[i - 4]) * scale2;
+                const int j = s0 + 8 * g + i - a.r;  // new row of the key, or committed
+                if (8 * g + i >= left || (j >= 0 && !((mask[rt] >> (j & 63)) & 1ull))) s[i] = -INFINITY;
+                mt = fmaxf(mt, s[i]);
+            }
+            if (__any(mt > m_run[rt] + LAZY)) move(rt_, mt);
+            float w[8], ps = 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                w[i] = s[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s[i] - m_run[rt]);
+                ps += w[i];
+                w[i] *= vs;
+            }
+            l_run[rt] += ps;
+            u32x4 p3[3];
+            split3(w, p3);
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                for (int p = 0; p < 3; ++p) o[rt][dt] = mfma_bf16(v[dt], p3[p], o[rt][dt]);
+            if (!odd) return;
+            // an infinity or NaN counts for the rows that see its key, and is nothing (not
+            // 0 x infinity) for the others
+#pragma unroll 1
+            for (int key = 0; key < left; ++key) {
+                float p = w[0];
+#pragma unroll
+                for (int i = 1; i < 8; ++i) p = (key & 7) == i ? w[i] : p;
+                p = __shfl(p, 16 * (key >> 3) + n);
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float x = bf2f(vt[(dt * 16 + 4 * g + j) * 32 + key]);
+                        if (!__builtin_isfinite(x) && p != 0.f) o[rt][dt][j] += p * x;
+                    }
+            }
+        });
     }
 
     // combine the waves (fixed order), one row tile at a time
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-        if (row0 + 16 * rt >= rows) break;  // (padding rows are of the last tile)
+    const __amdgpu_buffer_rsrc_t po = rsrc_of(a.part_o);
+    each<RT>([&](auto rt_) {
+        constexpr int rt = decltype(rt_)::value;
+        const int here = rows - row0 - 16 * rt;
+        if (here <= 0) return;  // (padding rows are of the last tile)
+        __syncthreads();
+        float l = l_run[rt];
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
         if (g == 0) {
             sm_m[wave][n] = m_run[rt];
-            sm_l[wave][n] = l_run[rt];
+            sm_l[wave][n] = l;
         }
+        const float u = v_unit / W_UNIT;
 #pragma unroll
-        for (int dt = 0; dt < ND; ++dt)
+        for (int dt = 0; dt < ND; ++dt) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) sm_o[wave][4 * g + j][dt * 16 + n] = o[rt][dt][j];
+            for (int j = 0; j < 4; ++j) o[rt][dt][j] *= u;
+            if (n < here) *reinterpret_cast<f32x4 *>(&sm_o[wave][n][dt * 16 + 4 * g]) = o[rt][dt];
+        }
         __syncthreads();
-        for (int e = threadIdx.x; e < 16 * (HD / 4); e += 256) {
+        for (int e = tid; e < 16 * (HD / 4); e += 64 * NW) {
             const int i = e / (HD / 4), d0 = 4 * (e % (HD / 4)), row = row0 + 16 * rt + i;
             if (row >= (a.n_split == 1 ? a.rows_out : rows)) continue;
             float mx = -INFINITY;
 #pragma unroll
             for (int w = 0; w < NW; ++w) mx = fmaxf(mx, sm_m[w][i]);
-            float l = 0.f, ov[4] = {0.f, 0.f, 0.f, 0.f};
+            float ls = 0.f, ov[4] = {0.f, 0.f, 0.f, 0.f};
+            if (i < here)
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
                 const float mw = sm_m[w][i], wgt = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - mx);
-                l = fmaf(wgt, sm_l[w][i], l);
+                ls = fmaf(wgt, sm_l[w][i], ls);
                 const f32x4 o4 = *reinterpret_cast<const f32x4 *>(&sm_o[w][i][d0]);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) ov[j] = fmaf(wgt, o4[j], ov[j]);
             }
             if (a.n_split == 1) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) ov[j] = l == 0.f ? 0.f : ov[j] / l;
+                for (int j = 0; j < 4; ++j) ov[j] = ls == 0.f ? 0.f : ov[j] / ls;
                 write_out(a, HD, h, row, d0, ov);
             } else {
-                const int64_t p = ((int64_t)h * a.n_split + split) * rows + row;
-                *reinterpret_cast<float4 *>(a.part_o + p * HD + d0) = make_float4(ov[0], ov[1], ov[2], ov[3]);
-                if (d0 == 0) {
-                    a.part_m[p] = mx;
-                    a.part_l[p] = l;
-                }
+                // published with device-coherent stores for the workgroup that combines
+                const uint32_t p = (uint32_t)((h * a.n_split + split) * rows + row);
+                const f32x4 o4 = {ov[0], ov[1], ov[2], ov[3]};
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o4), po, (p * HD + d0) * 4, 0, 16);
+                if (d0 == 0)
+                    __hip_atomic_store(a.part_ml + p, (uint64_t)__float_as_uint(ls) << 32 | __float_as_uint(mx), __ATOMIC_RELAXED,
+                                       __HIP_MEMORY_SCOPE_AGENT);
             }
         }
-        __syncthreads();
-    }
-}
+    });
+    if (a.n_split == 1) return;
 
-// The ranges of a row combined in their order, 4 dims per thread.
-template <int HD> __global__ __launch_bounds__(256) void k_kvq_merge(KvqAttnArgs a)
-{
-    const int rows = a.n * a.G, rows_out = a.rows_out;
-    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int d0 = 4 * (int)(e % (HD / 4));
-    const int64_t hr = e / (HD / 4);
-    if (hr >= (int64_t)a.H * rows_out) return;
-    const int h = (int)(hr / rows_out), row = (int)(hr - (int64_t)h * rows_out);
-    float m = -INFINITY, l = 0.f, ov[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < a.n_split && row < rows; ++s) {
-        const int64_t p = ((int64_t)h * a.n_split + s) * rows + row;
-        const float ms = a.part_m[p], ls = a.part_l[p];
-        const float4 o4 = *reinterpret_cast<const float4 *>(a.part_o + p * HD + d0);
-        if (ms == -INFINITY) {
-            // nothing seen in this range, or only NaN
-            l += ls;
-            continue;
+    // every workgroup waits for its own stores before it is counted, so the last one
+    // finds all of them
+    __shared__ int last;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    uint64_t *word = a.arrived + (h * gridDim.z + blockIdx.z) * KVQ_WORD;
+    if (tid == 0) last = last_of(word, a.tag, a.n_split);
+    __syncthreads();
+    if (!last) return;
+    // references of all ranges into LDS; their maximum and the rescaled sum, 16 lanes a row
+    constexpr int LR = 16;
+    static_assert(64 * NW >= LR * 16 * RT && sizeof sm >= 16 * RT * KVQ_MAX_SPLIT * 4, "a pass of the rows");
+    float *sm_ms = reinterpret_cast<float *>(sm);  // [rows][n_split]
+    __shared__ float sm_mx[16 * RT], sm_sum[16 * RT];
+    const int rows_here = min(16 * RT, rows - row0);
+    if (tid < LR * rows_here) {
+        const int row = tid / LR;
+        float m = -INFINITY, l = 0.f;
+        for (int s = tid % LR; s < a.n_split; s += LR) {
+            const uint64_t ml = __hip_atomic_load(a.part_ml + ((h * a.n_split + s) * rows + row0 + row), __ATOMIC_RELAXED,
+                                                  __HIP_MEMORY_SCOPE_AGENT);
+            const float ms = __uint_as_float((uint32_t)ml), ls = __uint_as_float((uint32_t)(ml >> 32));
+            sm_ms[row * a.n_split + s] = ms;
+            const float mx = fmaxf(m, ms);  // (a range that saw nothing, or only NaN, has no reference)
+            l = l * (m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mx)) +
+                ls * (ms == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ms - mx));
+            m = mx;
         }
-        const float mx = fmaxf(m, ms);
-        const float sc = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mx), w = __builtin_amdgcn_exp2f(ms - mx);
-        l = fmaf(w, ls, l * sc);
-        ov[0] = fmaf(w, o4.x, ov[0] * sc);
-        ov[1] = fmaf(w, o4.y, ov[1] * sc);
-        ov[2] = fmaf(w, o4.z, ov[2] * sc);
-        ov[3] = fmaf(w, o4.w, ov[3] * sc);
-        m = mx;
-    }
 #pragma unroll
-    for (int j = 0; j < 4; ++j) ov[j] = l == 0.f ? 0.f : ov[j] / l;
-    write_out(a, HD, h, row, d0, ov);
+        for (int off = 1; off < LR; off <<= 1) {
+            const float m2 = __shfl_xor(m, off), l2 = __shfl_xor(l, off), mx = fmaxf(m, m2);
+            l = l * (m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mx)) +
+                l2 * (m2 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m2 - mx));
+            m = mx;
+        }
+        if (tid % LR == 0) {
+            sm_mx[row] = m;
+            sm_sum[row] = l;
+        }
+    }
+    __syncthreads();
+    const int rows_end = row0 + rows_here == rows ? a.rows_out - row0 : rows_here;
+    constexpr int CH = 8;  // ranges whose loads are in flight together
+    for (int e = tid; e < rows_end * (HD / 4); e += 64 * NW) {
+        const int row = e / (HD / 4), d0 = 4 * (e % (HD / 4));
+        float ov[4] = {0.f, 0.f, 0.f, 0.f};
+        if (row < rows_here) {
+            const uint32_t p0 = (uint32_t)(h * a.n_split * rows + row0 + row);
+            const float mx = sm_mx[row], l = sm_sum[row];
+            for (int s0 = 0; s0 < a.n_split; s0 += CH) {
+                f32x4 os[CH];
+#pragma unroll
+                for (int c = 0; c < CH; ++c)
+                    os[c] = __builtin_bit_cast(
+                        f32x4, __builtin_amdgcn_raw_buffer_load_b128(po, ((p0 + min(s0 + c, a.n_split - 1) * rows) * HD + d0) * 4, 0, 16));
+#pragma unroll
+                for (int c = 0; c < CH; ++c) {
+                    const float ms = sm_ms[row * a.n_split + min(s0 + c, a.n_split - 1)];
+                    const float w = s0 + c >= a.n_split || ms == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms - mx);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) ov[j] = fmaf(w, os[c][j], ov[j]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) ov[j] = l == 0.f ? 0.f : ov[j] / l;
+        }
+        write_out(a, HD, h, row0 + row, d0, ov);
+    }
+    if (tid == 0) __hip_atomic_store(word, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
 template <int HD, bool F8> hipError_t attention(const KvqAttnArgs &a, const KvqCut &cut, hipStream_t s)
 {
     const dim3 grid(cut.n_split, a.H, cut.z);
-    switch (cut.rt) {
-    case 1: hipLaunchKernelGGL((k_kvq_attn<HD, F8, 1>), grid, dim3(256), 0, s, a); break;
-    case 2: hipLaunchKernelGGL((k_kvq_attn<HD, F8, 2>), grid, dim3(256), 0, s, a); break;
-    case 4: hipLaunchKernelGGL((k_kvq_attn<HD, F8, 4>), grid, dim3(256), 0, s, a); break;
-    default: return hipErrorInvalidValue;
-    }
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || cut.n_split == 1) return e;
-    const int64_t work = (int64_t)a.H * a.rows_out * (HD / 4);
-    hipLaunchKernelGGL(k_kvq_merge<HD>, dim3((unsigned)((work + 255) / 256)), dim3(256), 0, s, a);
+    if (cut.rt == 1)
+        hipLaunchKernelGGL((k_kvq_attn<HD, F8, 1, 8>), grid, dim3(512), 0, s, a);
+    else
+        hipLaunchKernelGGL((k_kvq_attn<HD, F8, 2, 8>), grid, dim3(512), 0, s, a);
     return hipGetLastError();
 }
 

@@ -263,19 +263,23 @@ def _sees(rng, n, kind):
 
 
 def _tolerance(q, k, v, sees):
-    """Bound of one head's error, [n].  u = 2^-24; products of exact operands.  A score
-    is a sum of 3 hd products added in fp32, in chunks of at least 4: it is off by at
-    most (3 hd / 4 + 8) u times the sum of |q k| / sqrt(hd), in which the 8 covers the
-    scale's, the factor's and the running maximum's roundings; exp2's argument adds 3 u of its
-    size and exp2 itself 2 u.  A weight's relative error is that; the sums over keys add
-    (keys + 16) u of the sum's absolute terms.  Numerator and denominator each."""
+    """Bound of one head's error, [n], worst cases added up; u = 2^-24, a half step of fp32.
+    A score: its query is cut to 2^-22 of the row's largest number (int8: an integer of
+    at most 2^22 rounded; e4m3: two truncated fp16 of a row scaled to at most 2^11), which
+    moves it by 4 u max|q| sum|k| / sqrt(hd); at most 3 hd products are added in fp32, by at
+    least 4 at a time, and scale, factor and reference round a few times: (3 hd / 4 + 16) u
+    times the sum of |q k| / sqrt(hd).  exp2 adds 2 u, a weight in two truncated fp16 is
+    cut by 4 u of it, or by 2^-24 / 2^11 of the largest, and V's scales round 4 times: 12 u
+    relative and 2^-35 of the largest weight per key.  The sums over keys: (keys + 16) u of
+    their absolute terms.  Numerator and denominator each."""
     u, (n, hd) = 2.0 ** -24, q.shape
     tol = np.zeros(n)
     for i in range(n):
         at = np.flatnonzero(sees[i])
         if len(at):
             mag = (np.abs(k[at]) @ np.abs(q[i])).max() / np.sqrt(hd)
-            rel = (3 * hd / 4 + 16) * u * mag + 4 * u + (len(at) + 16) * u
+            cut = 4 * u * np.abs(q[i]).max() * np.abs(k[at]).sum(axis=1).max() / np.sqrt(hd)
+            rel = cut + (3 * hd / 4 + 16) * u * mag + 12 * u + len(at) * 2.0 ** -35 + (len(at) + 16) * u
             tol[i] = 2 * rel * np.abs(v[at]).max()
     return tol
 
