@@ -3,8 +3,6 @@
 #include <hip/hip_runtime_api.h>
 
 #include <algorithm>
-#include <atomic>
-#include <chrono>
 #include <cstring>
 #include <mutex>
 
@@ -100,30 +98,18 @@ KvqAttnArgs attention_args(const dv_kvq *c, int layer, int n)
     a.blocks = c->len / KVQ_BLOCK;
     a.r = c->len % KVQ_BLOCK;
     a.n = n;
-    a.H = c->n_heads;
+    a.o.H = c->n_heads;
     a.tiles = a.blocks + (a.r + n + KVQ_BLOCK - 1) / KVQ_BLOCK;
     return a;
-}
-
-// A number that no other call of this process has, from a start that no memory holds
-// by chance; 48 bits, above a count's 16.
-uint64_t next_tag()
-{
-    static std::atomic<uint64_t> count{(uint64_t)std::chrono::steady_clock::now().time_since_epoch().count() * 0x9e3779b97f4a7c15ull >> 16};
-    return (count.fetch_add(1, std::memory_order_relaxed) | 1ull << 47) << 16;
 }
 
 // The cut, and its parts of the workspace.
 void set_cut(KvqAttnArgs &a, const KvqCut &cut, int hd, void *ws)
 {
-    const size_t rows = (size_t)a.H * cut.n_split * a.n * a.G;
     a.per_split = cut.per_split;
-    a.n_split = cut.n_split;
-    if (cut.n_split == 1) return;
-    a.arrived = static_cast<uint64_t *>(ws);
-    a.part_o = reinterpret_cast<float *>(static_cast<char *>(ws) + kvq_words_bytes(a.H, cut.z));
-    a.part_ml = reinterpret_cast<uint64_t *>(a.part_o + rows * hd);
-    a.tag = next_tag();
+    a.o.n_split = cut.n_split;
+    a.o.part_o = static_cast<float *>(ws);
+    a.o.part_ml = reinterpret_cast<float2 *>(a.o.part_o + (size_t)a.o.H * cut.n_split * a.o.rows * hd);
 }
 
 // The handle's step and prompts over an 8-bit cache: a step's nodes go to the tail
@@ -142,18 +128,19 @@ struct KvqSeam final : CacheSeam {
     hipError_t attend(const AttnArgs &s, int l) override
     {
         KvqAttnArgs a = attention_args(c, l, s.tm.M);
-        a.G = 1;
         a.q = s.q;
         a.ldq = (int64_t)s.H * s.hd;
-        a.out = s.out;
-        a.ldo = a.ldq;
-        a.out_split = s.out_split;
-        a.Mpad = s.tm.Mpad;
-        a.half = s.tm.half;
-        a.rows_out = s.out_split ? (s.tm.half ? 8 : s.tm.Mpad) : a.n;
+        a.o.G = 1;
+        a.o.rows = a.n;
+        a.o.rows_out = s.out_split ? (s.tm.half ? 8 : s.tm.Mpad) : a.n;
+        a.o.out = s.out;
+        a.o.ldo = a.ldq;
+        a.o.split = s.out_split;
+        a.o.Mpad = s.tm.Mpad;
+        a.o.half = s.tm.half;
         std::memcpy(a.mask, s.tm.anc, sizeof a.mask);
         // (the handle's partials hold 512 workgroups' sums of 64 rows)
-        const KvqCut cut = kvq_cut(a.H, a.n, a.tiles, std::min(h->n_cu, 256));
+        const KvqCut cut = kvq_cut(a.o.H, a.n, a.tiles, std::min(h->n_cu, 256));
         set_cut(a, cut, s.hd, h->part_o);
         return launch_kvq_attention(a, s.hd, c->format == DV_F8, cut, h->stream);
     }
@@ -289,15 +276,15 @@ int dv_kvq_attention(const dv_kvq *c, int32_t layer, const float *q, int64_t q_s
     hipError_t e = current_cus(&n_cu);
     if (e != hipSuccess) return set_err(nullptr, DV_EHIP, "compute units: %s", hipGetErrorString(e));
     KvqAttnArgs a = attention_args(c, layer, n);
-    a.G = n_heads / c->n_heads;
-    a.rows_out = n * a.G;
     a.q = q;
     a.ldq = q_stride;
-    a.out = out;
-    a.ldo = out_stride;
+    a.o.G = n_heads / c->n_heads;
+    a.o.rows = a.o.rows_out = n * a.o.G;
+    a.o.out = out;
+    a.o.ldo = out_stride;
     for (int i = 0; i < n; ++i) a.mask[i] = mask ? mask[i] : ~0ull >> (63 - i);
-    const KvqCut cut = kvq_cut(a.H, n * a.G, a.tiles, n_cu);
-    const size_t need = kvq_attention_bytes(a.H, n * a.G, c->head_dim, cut.n_split);
+    const KvqCut cut = kvq_cut(a.o.H, a.o.rows, a.tiles, n_cu);
+    const size_t need = kvq_attention_bytes(a.o.H, a.o.rows, c->head_dim, cut.n_split);
     if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < 0 || (size_t)workspace_bytes < need))
         return set_err(nullptr, DV_EINVAL, "attention needs a 16-byte aligned workspace of %zu bytes", need);
     set_cut(a, cut, c->head_dim, workspace);

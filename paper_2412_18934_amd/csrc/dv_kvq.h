@@ -4,14 +4,13 @@
 #pragma once
 
 #include <hip/hip_runtime_api.h>
+#include <hip/hip_vector_types.h>
 #include <stddef.h>
 #include <stdint.h>
 
 #define KVQ_BLOCK 32      // slots that share a scale
 #define KVQ_TAIL 96       // bf16 slots per head behind the last whole block: 31 committed + 64 new
 #define KVQ_MAX_NEW 64    // new rows of one call
-#define KVQ_MAX_SPLIT 256 // ranges of a head's keys
-#define KVQ_WORD 16       // 8-byte words from one counter to the next: counters of one line queue up
 
 // Consecutive layers of a cache (L of them, from the pointers' layer on).
 struct KvqLayers {
@@ -48,7 +47,7 @@ inline int kvq_row_groups(int rows) { return (rows + 16 * kvq_row_tiles(rows) - 
 inline int kvq_max_split(int heads, int rows, int n_cu)
 {
     const int most = n_cu / (heads * kvq_row_groups(rows));
-    return most < 1 ? 1 : most > KVQ_MAX_SPLIT ? KVQ_MAX_SPLIT : most;
+    return most > 1 ? most : 1;
 }
 inline KvqCut kvq_cut(int heads, int rows, int tiles, int n_cu)
 {
@@ -61,15 +60,25 @@ inline KvqCut kvq_cut(int heads, int rows, int tiles, int n_cu)
     c.n_split = (tiles + c.per_split - 1) / c.per_split;
     return c;
 }
-// Workspace of n_split ranges (one writes the output itself): a word of arrivals for
-// each head and row group, then the partial sums, references and weights.
-inline size_t kvq_words_bytes(int heads, int z) { return (size_t)heads * z * KVQ_WORD * 8; }
+// Workspace of n_split ranges (one writes the output itself): partial sums, and a
+// reference and sum of weights for each.
 inline size_t kvq_attention_bytes(int heads, int rows, int hd, int n_split)
 {
-    if (n_split == 1) return 0;
-    return kvq_words_bytes(heads, kvq_row_groups(rows)) + (size_t)heads * n_split * rows * (hd + 2) * 4;
+    return n_split == 1 ? 0 : (size_t)heads * n_split * rows * (hd + 2) * 4;
 }
 
+// Where attention's sums go: the output, or ranges to be combined.
+struct KvqOut {
+    float *out;                  // [n][H G][hd], row stride ldo, or
+    int64_t ldo;
+    uint16_t *split;             // the split layout of a step's activations (Mpad, half)
+    int32_t Mpad, half;
+    int32_t H, G;                // KV heads, query heads per KV head
+    int32_t rows, rows_out;      // n G; those to write: with the split layout its padding too (zeros)
+    int32_t n_split;
+    float *part_o;               // [H][n_split][rows][hd] unnormalised sums
+    float2 *part_ml;             // [H][n_split][rows]: reference (base 2) and sum of weights
+};
 struct KvqAttnArgs {
     const uint8_t *k, *v;        // this layer's codes, scales, tail
     const float *scale;
@@ -77,19 +86,10 @@ struct KvqAttnArgs {
     int32_t nb;                  // blocks per head (the stride)
     int32_t blocks;              // whole blocks committed
     int32_t r, n;                // committed and new rows of the tail
-    int32_t H, G;                // KV heads, query heads per KV head
     const float *q;              // [n][H G][hd], row stride ldq
     int64_t ldq;
-    float *out;                  // [n][H G][hd], row stride ldo, or
-    int64_t ldo;
-    uint16_t *out_split;         // the split layout of a step's activations (Mpad, half)
-    int32_t Mpad, half;
-    int32_t rows_out;            // rows to write: n G, or with out_split its padding too (zeros)
-    int32_t tiles, per_split, n_split;
-    float *part_o;               // [H][n_split][rows][hd] unnormalised sums
-    uint64_t *part_ml;           // [H][n_split][rows]: reference and sum of weights
-    uint64_t *arrived;           // [H][row groups]
-    uint64_t tag;                // this call's, in the upper 48 bits
+    int32_t tiles, per_split;
+    KvqOut o;
     uint64_t mask[KVQ_MAX_NEW];  // bit j: new row i sees new row j
 };
 hipError_t launch_kvq_attention(const KvqAttnArgs &a, int hd, int f8, const KvqCut &cut, hipStream_t s);

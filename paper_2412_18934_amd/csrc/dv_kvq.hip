@@ -353,9 +353,9 @@ template <bool F8, int HD> __global__ __launch_bounds__(256) void k_kvq_advance(
 //
 // Workgroup (split, KV head, row group): its waves take interleaved 32-key tiles of
 // the range (blocks of codes, then up to three tiles of the tail) with a running
-// reference m and sum per query row, and are combined in LDS; the last range of a
-// head and row group to finish combines the ranges, in their order.  Rows are the n
-// new tokens x the G query heads that share the KV head.
+// reference m and sum per query row, and are combined in LDS; a second launch combines
+// the ranges, in their order.  Rows are the n new tokens x the G query heads that share
+// the KV head.
 //
 //   S^T = K Q^T: A = 16 keys x dims, B = queries; D gives lane (n, g) the scores of
 //   row n for the 8 consecutive keys 8 g .. +8 of the tile, which are the B operand
@@ -439,6 +439,12 @@ __device__ __forceinline__ void split2(const float *v, u32x4 (&t)[2])
     }
 }
 
+__device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b)
+{
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
+}
+
 __device__ __forceinline__ f32x4 mfma_bf16(const u32x4 &a, const u32x4 &b, const f32x4 &c)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -453,31 +459,13 @@ __device__ __forceinline__ i32x4 mfma_i8(const u32x4 &a, const u32x4 &b, const i
 }
 
 // Row `row` of KV head h is query head h G + row % G of token row / G.
-__device__ __forceinline__ void write_out(const KvqAttnArgs &a, int hd, int h, int row, int d0, const float (&o)[4])
+__device__ __forceinline__ void write_out(const KvqOut &a, int hd, int h, int row, int d0, const float (&o)[4])
 {
     const int i = row / a.G, col = (h * a.G + row % a.G) * hd + d0;
-    if (a.out_split)
-        store_split4(a.out_split, i, col, split_mt(a.Mpad, a.half), make_float4(o[0], o[1], o[2], o[3]));
+    if (a.split)
+        store_split4(a.split, i, col, split_mt(a.Mpad, a.half), make_float4(o[0], o[1], o[2], o[3]));
     else
         *reinterpret_cast<float4 *>(a.out + i * a.ldo + col) = make_float4(o[0], o[1], o[2], o[3]);
-}
-
-// Whether this is the last of n workgroups to get here, each once.  The word may
-// start as anything: it counts under the call's tag (48 bits, the count below them).
-// A workgroup that does not find the tag sets it, with itself as the first, or finds
-// it set by another one and is counted then; one that finds it has been counted.
-__device__ __forceinline__ bool last_of(uint64_t *w, uint64_t tag, int n)
-{
-    uint64_t old = __hip_atomic_fetch_add(w, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    while (old >> 16 != tag >> 16) {
-        uint64_t cur = __hip_atomic_load(w, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        if (cur >> 16 == tag >> 16)
-            old = __hip_atomic_fetch_add(w, 1ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        else if (__hip_atomic_compare_exchange_strong(w, &cur, tag | 1, __ATOMIC_RELAXED, __ATOMIC_RELAXED,
-                                                      __HIP_MEMORY_SCOPE_AGENT))
-            old = tag;
-    }
-    return (int)(old & 0xffff) == n - 1;
 }
 
 // f(0), .. f(N - 1) with constant arguments: a row tile's registers are never indexed
@@ -496,16 +484,16 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
     constexpr int NT = 3 * NC;                       // and for the tail
     const int split = blockIdx.x, h = blockIdx.y, row0 = blockIdx.z * 16 * RT;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
-    const int rows = a.n * a.G;
+    const int rows = a.n * a.o.G;
     constexpr float scale2 = HD == 128 ? 1.4426950408889634f / 11.313708498984761f : 1.4426950408889634f / 8.f;
 
     // query parts as operands; later the waves' sums
-    constexpr int SUMS = NW * 16 * (HD + 4) * 4, PARTS = RT * (NQ + NT) * 1024;
+    constexpr int SUMS = NW * 16 * RT * (HD + 4) * 4, PARTS = RT * (NQ + NT) * 1024;
     __shared__ __align__(16) char sm[SUMS > PARTS ? SUMS : PARTS];
-    __shared__ float sm_m[NW][16], sm_l[NW][16], sm_c[16 * RT];
+    __shared__ float sm_m[NW][16 * RT], sm_l[NW][16 * RT], sm_c[16 * RT];
     u32x4(*qc)[NQ * 64] = reinterpret_cast<u32x4(*)[NQ * 64]>(sm);
     u32x4(*qt)[NT * 64] = reinterpret_cast<u32x4(*)[NT * 64]>(sm + RT * NQ * 1024);
-    float(*sm_o)[16][HD + 4] = reinterpret_cast<float(*)[16][HD + 4]>(sm);
+    float(*sm_o)[16 * RT][HD + 4] = reinterpret_cast<float(*)[16 * RT][HD + 4]>(sm);
 
     struct Raw {
         u32x4 k[NC], v[NC];
@@ -530,11 +518,44 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
     const int d8 = tid % (HD / 8), qrow = tid / (HD / 8);
     float4 qx = make_float4(0.f, 0.f, 0.f, 0.f), qy = qx;
     if (qrow < RT * 16 && row0 + qrow < rows) {
-        const float *p = a.q + ((row0 + qrow) / a.G) * a.ldq + (h * a.G + (row0 + qrow) % a.G) * HD + d8 * 8;
+        const float *p = a.q + ((row0 + qrow) / a.o.G) * a.ldq + (h * a.o.G + (row0 + qrow) % a.o.G) * HD + d8 * 8;
         qx = *reinterpret_cast<const float4 *>(p);
         qy = *reinterpret_cast<const float4 *>(p + 4);
     }
-    if (t0 + wave < c1) load(t0 + wave, buf0);
+    // a tile of the tail in the same registers: 16 bytes per lane and load, strides k_step
+    // (K) and 1 KB (V)
+    auto tail_at = [&](int t, const char *&k0, const char *&k1, const char *&v0) {
+        const int s0 = (t - a.blocks) * KVQ_BLOCK;
+        const uint16_t *kp = a.kt + ((int64_t)h * KVQ_TAIL + s0) * HD + 8 * g;
+        k0 = reinterpret_cast<const char *>(kp + k_slot(lane, 0) * HD);
+        k1 = reinterpret_cast<const char *>(kp + k_slot(lane, 1) * HD);
+        v0 = reinterpret_cast<const char *>(a.vt + ((int64_t)h * KVQ_TAIL + s0) * HD + n * 32 + 8 * g);
+    };
+    auto fetch = [&](const char *kp, int k_step, const char *vp, Raw &x) {
+#pragma unroll
+        for (int j = 0; j < NC; ++j) x.k[j] = *reinterpret_cast<const u32x4 *>(kp + j * k_step);
+#pragma unroll
+        for (int j = 0; j < NC; ++j) x.v[j] = *reinterpret_cast<const u32x4 *>(vp + j * 1024);
+    };
+    auto load_tail = [&](int t) {
+        const char *k0, *k1, *v0;
+        tail_at(t, k0, k1, v0);
+        fetch(k0, 64, v0, buf0);
+        fetch(k1, 64, v0 + NC * 1024, buf1);
+    };
+    // The wave's first tile, codes or tail, without a branch: the queries' wait then leaves
+    // these loads in flight.  (A wave without a tile takes the range's first, which is
+    // somewhere in the buffers, and does not use it.)
+    const bool tail_first = t0 + wave >= c1;
+    {
+        const char *k0, *k1, *v0;
+        tail_at(max(min(t0 + wave, t1 - 1), a.blocks), k0, k1, v0);
+        const int64_t at = (int64_t)h * a.nb + (tail_first ? 0 : t0 + wave);
+        const char *kc = reinterpret_cast<const char *>(a.k + at * KVQ_BLOCK * HD + lane * 16);
+        const char *vc = reinterpret_cast<const char *>(a.v + at * KVQ_BLOCK * HD + lane * 16);
+        buf0.s = *reinterpret_cast<const float2 *>(a.scale + at * 2);
+        fetch(tail_first ? k0 : kc, tail_first ? 64 : 1024, tail_first ? v0 : vc, buf0);
+    }
     if (qrow < RT * 16) {
         const int row = qrow, c = d8 >> 2, at = 16 * (d8 & 3) + row % 16;
         const float v[8] = {qx.x, qx.y, qx.z, qx.w, qy.x, qy.y, qy.z, qy.w};
@@ -579,11 +600,17 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
             for (int p = 0; p < 3; ++p) qt[row / 16][(c * 3 + p) * 64 + at] = t[p];
         }
     }
+    if (t0 + wave + NW < c1) load(t0 + wave + NW, buf1);
+    if (tail_first && t0 + wave < t1) {
+        const char *k0, *k1, *v0;
+        tail_at(t0 + wave, k0, k1, v0);
+        fetch(k1, 64, v0 + NC * 1024, buf1);
+    }
     uint64_t mask[RT];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         const int row = row0 + 16 * rt + n;
-        mask[rt] = has_tail && row < rows ? a.mask[row / a.G] : 0ull;
+        mask[rt] = has_tail && row < rows ? a.mask[row / a.o.G] : 0ull;
     }
     __syncthreads();
 
@@ -695,44 +722,46 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
             }
         });
     };
-    // two buffers in turn: the next tile loads while one is used
+    // two buffers in turn: a tile loads while the other is used
     for (int t = t0 + wave; t < c1; t += 2 * NW) {
-        if (t + NW < c1) load(t + NW, buf1);
         codes(buf0);
-        if (t + NW >= c1) break;
         if (t + 2 * NW < c1) load(t + 2 * NW, buf0);
+        if (t + NW >= c1) break;
         codes(buf1);
+        if (t + 3 * NW < c1) load(t + 3 * NW, buf1);
     }
 
     // tail tiles of the range, by the waves whose turn it is
     const int tt = max(t0, a.blocks);
     for (int t = tt + (wave + NW - (tt - t0) % NW) % NW; t < t1; t += NW) {
         const int s0 = (t - a.blocks) * KVQ_BLOCK, left = min(KVQ_BLOCK, a.r + a.n - s0);
-        const uint16_t *kp = a.kt + ((int64_t)h * KVQ_TAIL + s0) * HD + 8 * g;
         const uint16_t *vt = a.vt + ((int64_t)h * KVQ_TAIL + s0) * HD;
-        u32x4 ka[NC], kb[NC], v[ND];
+        if (t != t0 + wave) load_tail(t);
+        u32x4 v[ND];
+        // V without the slots past the last row, which hold anything
+        const int mine = min(max(left - 8 * g, 0), 8);  // of the lane's 8 keys
+        uint32_t keep[4], top = 0;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            ka[c] = *reinterpret_cast<const u32x4 *>(kp + k_slot(lane, 0) * HD + 32 * c);
-            kb[c] = *reinterpret_cast<const u32x4 *>(kp + k_slot(lane, 1) * HD + 32 * c);
-        }
-        // V without the slots past the last row, which hold anything, and without its
-        // infinities and NaN, which come after
-        bool odd = false;
+        for (int w = 0; w < 4; ++w) keep[w] = (2 * w < mine ? 0xffffu : 0u) | (2 * w + 1 < mine ? 0xffff0000u : 0u);
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) {
-            v[dt] = *reinterpret_cast<const u32x4 *>(vt + (dt * 16 + n) * 32 + 8 * g);
+            v[dt] = dt < NC ? buf0.v[dt % NC] : buf1.v[dt % NC];
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
-                uint32_t x = v[dt][w];
-                if (8 * g + 2 * w >= left) x = 0u;
-                else if (8 * g + 2 * w + 1 >= left) x &= 0xffffu;
-                const uint32_t is = ((x & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((x & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u);
-                v[dt][w] = x & ~is;
-                odd |= is != 0u;
+                v[dt][w] &= keep[w];
+                top = max_u16x2(top, v[dt][w] & 0x7fff7fffu);
             }
         }
-        odd = __any(odd);
+        // infinities and NaN are taken out as well, and come after
+        const bool odd = __any((top & 0xffffu) >= 0x7f80u || top >= 0x7f800000u);
+        if (odd)
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    if ((v[dt][w] & 0x7f80u) == 0x7f80u) v[dt][w] &= 0xffff0000u;
+                    if ((v[dt][w] & 0x7f800000u) == 0x7f800000u) v[dt][w] &= 0xffffu;
+                }
         if (v_unit == 0.f) v_unit = v_inv = 1.f;  // no sums yet, or only zeros
         const float vs = v_inv * W_UNIT;
         each<RT>([&](auto rt_) {
@@ -742,15 +771,17 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
 #pragma unroll
             for (int c = 0; c < NT; ++c) {
                 const u32x4 q = qt[rt][c * 64 + lane];
-                sa = mfma_bf16(ka[c / 3], q, sa);
-                sb = mfma_bf16(kb[c / 3], q, sb);
+                sa = mfma_bf16(buf0.k[c / 3], q, sa);
+                sb = mfma_bf16(buf1.k[c / 3], q, sb);
             }
+            // bit i: the row sees the lane's key i, committed or new row first + i
+            const int first = s0 + 8 * g - a.r;
+            const uint32_t see = (first >= 0 ? (uint32_t)(mask[rt] >> (first & 63))
+                                  : first > -8 ? (uint32_t)mask[rt] << -first | (1u << -first) - 1 : 0xffu) & ((1u << mine) - 1);
             float s[8], mt = -INFINITY;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                s[i] = (i < 4 ? sa[i] : sb[i - 4]) * scale2;
-                const int j = s0 + 8 * g + i - a.r;  // new row of the key, or committed
-                if (8 * g + i >= left || (j >= 0 && !((mask[rt] >> (j & 63)) & 1ull))) s[i] = -INFINITY;
+                s[i] = see >> i & 1 ? (i < 4 ? sa[i] : sb[i - 4]) * scale2 : -INFINITY;
                 mt = fmaxf(mt, s[i]);
             }
             if (__any(mt > m_run[rt] + LAZY)) move(rt_, mt);
@@ -788,36 +819,37 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
         });
     }
 
-    // combine the waves (fixed order), one row tile at a time
-    const __amdgpu_buffer_rsrc_t po = rsrc_of(a.part_o);
+    // combine the waves, in their order
+    const int rows_here = min(16 * RT, rows - row0);
+    const int rows_end = row0 + rows_here == rows ? a.o.rows_out - row0 : rows_here;  // with padding
+    __syncthreads();
     each<RT>([&](auto rt_) {
         constexpr int rt = decltype(rt_)::value;
-        const int here = rows - row0 - 16 * rt;
-        if (here <= 0) return;  // (padding rows are of the last tile)
-        __syncthreads();
         float l = l_run[rt];
         l += __shfl_xor(l, 16);
         l += __shfl_xor(l, 32);
+        if (16 * rt + n >= rows_here) return;
         if (g == 0) {
-            sm_m[wave][n] = m_run[rt];
-            sm_l[wave][n] = l;
+            sm_m[wave][16 * rt + n] = m_run[rt];
+            sm_l[wave][16 * rt + n] = l;
         }
         const float u = v_unit / W_UNIT;
 #pragma unroll
         for (int dt = 0; dt < ND; ++dt) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) o[rt][dt][j] *= u;
-            if (n < here) *reinterpret_cast<f32x4 *>(&sm_o[wave][n][dt * 16 + 4 * g]) = o[rt][dt];
+            *reinterpret_cast<f32x4 *>(&sm_o[wave][16 * rt + n][dt * 16 + 4 * g]) = o[rt][dt];
         }
-        __syncthreads();
-        for (int e = tid; e < 16 * (HD / 4); e += 64 * NW) {
-            const int i = e / (HD / 4), d0 = 4 * (e % (HD / 4)), row = row0 + 16 * rt + i;
-            if (row >= (a.n_split == 1 ? a.rows_out : rows)) continue;
-            float mx = -INFINITY;
+    });
+    __syncthreads();
+#pragma unroll
+    for (int e0 = 0; e0 < 16 * RT * (HD / 4); e0 += 64 * NW) {
+        const int i = (e0 + tid) / (HD / 4), d0 = 4 * (tid % (HD / 4));
+        if (i >= (a.o.n_split == 1 ? rows_end : rows_here)) break;
+        float mx = -INFINITY, ls = 0.f, ov[4] = {0.f, 0.f, 0.f, 0.f};
+        if (i < rows_here) {
 #pragma unroll
             for (int w = 0; w < NW; ++w) mx = fmaxf(mx, sm_m[w][i]);
-            float ls = 0.f, ov[4] = {0.f, 0.f, 0.f, 0.f};
-            if (i < here)
 #pragma unroll
             for (int w = 0; w < NW; ++w) {
                 const float mw = sm_m[w][i], wgt = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - mx);
@@ -826,101 +858,78 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) ov[j] = fmaf(wgt, o4[j], ov[j]);
             }
-            if (a.n_split == 1) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) ov[j] = ls == 0.f ? 0.f : ov[j] / ls;
-                write_out(a, HD, h, row, d0, ov);
-            } else {
-                // published with device-coherent stores for the workgroup that combines
-                const uint32_t p = (uint32_t)((h * a.n_split + split) * rows + row);
-                const f32x4 o4 = {ov[0], ov[1], ov[2], ov[3]};
-                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, o4), po, (p * HD + d0) * 4, 0, 16);
-                if (d0 == 0)
-                    __hip_atomic_store(a.part_ml + p, (uint64_t)__float_as_uint(ls) << 32 | __float_as_uint(mx), __ATOMIC_RELAXED,
-                                       __HIP_MEMORY_SCOPE_AGENT);
-            }
         }
-    });
-    if (a.n_split == 1) return;
+        if (a.o.n_split == 1) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) ov[j] = ls == 0.f ? 0.f : ov[j] / ls;
+            write_out(a.o, HD, h, row0 + i, d0, ov);
+        } else {
+            const int64_t p = ((int64_t)h * a.o.n_split + split) * rows + row0 + i;
+            *reinterpret_cast<float4 *>(a.o.part_o + p * HD + d0) = make_float4(ov[0], ov[1], ov[2], ov[3]);
+            if (d0 == 0) a.o.part_ml[p] = make_float2(mx, ls);
+        }
+    }
+}
 
-    // every workgroup waits for its own stores before it is counted, so the last one
-    // finds all of them
-    __shared__ int last;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-    uint64_t *word = a.arrived + (h * gridDim.z + blockIdx.z) * KVQ_WORD;
-    if (tid == 0) last = last_of(word, a.tag, a.n_split);
-    __syncthreads();
-    if (!last) return;
-    // references of all ranges into LDS; their maximum and the rescaled sum, 16 lanes a row
-    constexpr int LR = 16;
-    static_assert(64 * NW >= LR * 16 * RT && sizeof sm >= 16 * RT * KVQ_MAX_SPLIT * 4, "a pass of the rows");
-    float *sm_ms = reinterpret_cast<float *>(sm);  // [rows][n_split]
-    __shared__ float sm_mx[16 * RT], sm_sum[16 * RT];
-    const int rows_here = min(16 * RT, rows - row0);
-    if (tid < LR * rows_here) {
-        const int row = tid / LR;
-        float m = -INFINITY, l = 0.f;
-        for (int s = tid % LR; s < a.n_split; s += LR) {
-            const uint64_t ml = __hip_atomic_load(a.part_ml + ((h * a.n_split + s) * rows + row0 + row), __ATOMIC_RELAXED,
-                                                  __HIP_MEMORY_SCOPE_AGENT);
-            const float ms = __uint_as_float((uint32_t)ml), ls = __uint_as_float((uint32_t)(ml >> 32));
-            sm_ms[row * a.n_split + s] = ms;
+// The ranges combined, in a launch of its own: 4 threads share a row's 4 dims, each with
+// every fourth range, and are combined in LDS.
+template <int HD> __global__ __launch_bounds__(256) void k_kvq_merge(KvqOut a)
+{
+    constexpr int D4 = HD / 4, NR = 64 / D4;  // rows of a workgroup
+    __shared__ __align__(16) f32x4 sm_o[4][64];
+    __shared__ float sm_m[4][64], sm_l[4][64];
+    const int part = threadIdx.x >> 6, lane = threadIdx.x & 63, d0 = 4 * (lane % D4);
+    const int64_t hr = (int64_t)blockIdx.x * NR + lane / D4;
+    const int rows = a.rows, h = (int)(hr / a.rows_out), row = (int)(hr - (int64_t)h * a.rows_out);
+    const bool real = h < a.H && row < rows;
+    float m = -INFINITY, l = 0.f, ov[4] = {0.f, 0.f, 0.f, 0.f};
+    if (real)
+#pragma unroll 8
+        for (int s = part; s < a.n_split; s += 4) {
+            const int64_t p = ((int64_t)h * a.n_split + s) * rows + row;
+            const float2 ml = a.part_ml[p];
+            const f32x4 o4 = *reinterpret_cast<const f32x4 *>(a.part_o + p * HD + d0);
+            const float ms = ml.x, ls = ml.y;
             const float mx = fmaxf(m, ms);  // (a range that saw nothing, or only NaN, has no reference)
-            l = l * (m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mx)) +
-                ls * (ms == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ms - mx));
-            m = mx;
-        }
+            const float f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mx);
+            const float w = ms == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ms - mx);
+            l = l * f + w * ls;
 #pragma unroll
-        for (int off = 1; off < LR; off <<= 1) {
-            const float m2 = __shfl_xor(m, off), l2 = __shfl_xor(l, off), mx = fmaxf(m, m2);
-            l = l * (m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mx)) +
-                l2 * (m2 == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m2 - mx));
+            for (int j = 0; j < 4; ++j) ov[j] = ov[j] * f + w * o4[j];
             m = mx;
         }
-        if (tid % LR == 0) {
-            sm_mx[row] = m;
-            sm_sum[row] = l;
-        }
-    }
+    sm_m[part][lane] = m;
+    sm_l[part][lane] = l;
+    sm_o[part][lane] = (f32x4){ov[0], ov[1], ov[2], ov[3]};
     __syncthreads();
-    const int rows_end = row0 + rows_here == rows ? a.rows_out - row0 : rows_here;
-    constexpr int CH = 8;  // ranges whose loads are in flight together
-    for (int e = tid; e < rows_end * (HD / 4); e += 64 * NW) {
-        const int row = e / (HD / 4), d0 = 4 * (e % (HD / 4));
-        float ov[4] = {0.f, 0.f, 0.f, 0.f};
-        if (row < rows_here) {
-            const uint32_t p0 = (uint32_t)(h * a.n_split * rows + row0 + row);
-            const float mx = sm_mx[row], l = sm_sum[row];
-            for (int s0 = 0; s0 < a.n_split; s0 += CH) {
-                f32x4 os[CH];
+    if (part || h >= a.H) return;
 #pragma unroll
-                for (int c = 0; c < CH; ++c)
-                    os[c] = __builtin_bit_cast(
-                        f32x4, __builtin_amdgcn_raw_buffer_load_b128(po, ((p0 + min(s0 + c, a.n_split - 1) * rows) * HD + d0) * 4, 0, 16));
+    for (int p = 1; p < 4; ++p) {
+        const float ms = sm_m[p][lane], mx = fmaxf(m, ms);
+        const f32x4 o4 = sm_o[p][lane];
+        const float f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mx);
+        const float w = ms == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ms - mx);
+        l = l * f + w * sm_l[p][lane];
 #pragma unroll
-                for (int c = 0; c < CH; ++c) {
-                    const float ms = sm_ms[row * a.n_split + min(s0 + c, a.n_split - 1)];
-                    const float w = s0 + c >= a.n_split || ms == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ms - mx);
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) ov[j] = fmaf(w, os[c][j], ov[j]);
-                }
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) ov[j] = l == 0.f ? 0.f : ov[j] / l;
-        }
-        write_out(a, HD, h, row0 + row, d0, ov);
+        for (int j = 0; j < 4; ++j) ov[j] = ov[j] * f + w * o4[j];
+        m = mx;
     }
-    if (tid == 0) __hip_atomic_store(word, 0ull, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) ov[j] = l == 0.f ? 0.f : ov[j] / l;
+    write_out(a, HD, h, row, d0, ov);
 }
 
 template <int HD, bool F8> hipError_t attention(const KvqAttnArgs &a, const KvqCut &cut, hipStream_t s)
 {
-    const dim3 grid(cut.n_split, a.H, cut.z);
+    const dim3 grid(cut.n_split, a.o.H, cut.z);
     if (cut.rt == 1)
         hipLaunchKernelGGL((k_kvq_attn<HD, F8, 1, 8>), grid, dim3(512), 0, s, a);
     else
         hipLaunchKernelGGL((k_kvq_attn<HD, F8, 2, 8>), grid, dim3(512), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || cut.n_split == 1) return e;
+    const int64_t rows = (int64_t)a.o.H * a.o.rows_out, each = 256 / HD;
+    hipLaunchKernelGGL(k_kvq_merge<HD>, dim3((unsigned)((rows + each - 1) / each)), dim3(256), 0, s, a.o);
     return hipGetLastError();
 }
 

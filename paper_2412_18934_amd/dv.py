@@ -316,13 +316,14 @@ def dv_kvq_attention(kvq: dv_kvq, layer: int, q: int, q_stride: int, n: int, n_h
                      out_stride: int, workspace: int = 0, workspace_bytes: int = 0, stream: int = 0):
     """q / out / workspace: device addresses, strides in floats; mask: host array of
     n uint64, or None (row i sees new rows 0..i)."""
-    m = None
+    at = None
     if mask is not None:
-        m = np.ascontiguousarray(mask, dtype=np.uint64)
-        if len(m) < n:
+        mask = np.ascontiguousarray(mask, dtype=np.uint64)
+        if len(mask) < n:
             raise ValueError("mask needs one entry per row")
-    _check(lib().dv_kvq_attention(kvq, layer, q or None, q_stride, n, n_heads, None if m is None else m.ctypes.data,
-                                  out or None, out_stride, workspace or None, workspace_bytes, stream or None), None)
+        at = mask.__array_interface__["data"][0]
+    _check(lib().dv_kvq_attention(kvq, layer, q or None, q_stride, n, n_heads, at, out or None, out_stride,
+                                  workspace or None, workspace_bytes, stream or None), None)
 
 
 def dv_verify_step_kvq(h, tokens, tree_parents, kvq: dv_kvq, out_logits: int = 0) -> dv_accept:
