@@ -83,6 +83,12 @@ template <bool F8> __device__ __forceinline__ uint2 codes8(const u32x4 &x, float
     return make_uint2(d[0], d[1]);
 }
 
+template <bool F8> __device__ __forceinline__ void put_codes(const u32x4 &x, const u32x4 &y, float inv, uint8_t *to)
+{
+    const uint2 lo = codes8<F8>(x, inv), hi = codes8<F8>(y, inv);
+    *reinterpret_cast<u32x4 *>(to) = (u32x4){lo.x, lo.y, hi.x, hi.y};
+}
+
 // Eight codes as bf16, exact: int8 has 8 significant bits, e4m3 four and exponents
 // of -9 to 8.
 template <bool F8> __device__ __forceinline__ u32x4 bf16_of(uint32_t lo, uint32_t hi)
@@ -133,11 +139,27 @@ __device__ __forceinline__ void quantise(Get get, uint8_t *codes, float *scale, 
     for (int j = 0; j < NJ; ++j) m = max_bits(max_bits(m, x[j][0]), x[j][1]);
     const BlockScale b = block_scale<F8>(wave_max(m));
 #pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-        const uint2 lo = codes8<F8>(x[j][0], b.inv), hi = codes8<F8>(x[j][1], b.inv);
-        *reinterpret_cast<u32x4 *>(codes + (j * 64 + lane) * 16) = (u32x4){lo.x, lo.y, hi.x, hi.y};
-    }
+    for (int j = 0; j < NJ; ++j)
+        put_codes<F8>(x[j][0], x[j][1], b.inv, codes + (j * 64 + lane) * 16);
     if (lane == 0) *scale = b.scale;
+}
+
+// Slots [s0, s1) of eight slots of a dim of V, the first of them s; the others stay.
+__device__ __forceinline__ void copy_slots(uint16_t *to, const uint16_t *from, int s, int s0, int s1)
+{
+    if (s >= s1 || s + 8 <= s0) return;
+    u32x4 x = *reinterpret_cast<const u32x4 *>(from);
+    if (s < s0 || s + 8 > s1) {
+        const u32x4 y = *reinterpret_cast<const u32x4 *>(to);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t take = 0;
+            if (s + 2 * i >= s0 && s + 2 * i < s1) take |= 0xffffu;
+            if (s + 2 * i + 1 >= s0 && s + 2 * i + 1 < s1) take |= 0xffff0000u;
+            x[i] = (x[i] & take) | (y[i] & ~take);
+        }
+    }
+    *reinterpret_cast<u32x4 *>(to) = x;
 }
 
 // ---------------------------------------------------------------------------
@@ -201,19 +223,8 @@ template <bool F8, int HD> __global__ __launch_bounds__(256) void k_kvq_store(St
     if (s1 <= s0) return;
     if (is_v) {
         const uint16_t *tile = rows + (size_t)b1 * KVQ_BLOCK * HD;
-        for (int e = lane; e < HD * 4; e += 64) {
-            const int s = 8 * (e & 3);
-            if (s >= s1 || s + 8 <= s0) continue;
-            u32x4 x = *reinterpret_cast<const u32x4 *>(tile + e * 8), y = *reinterpret_cast<const u32x4 *>(tail + e * 8);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                uint32_t take = 0;
-                if (s + 2 * i >= s0 && s + 2 * i < s1) take |= 0xffffu;
-                if (s + 2 * i + 1 >= s0 && s + 2 * i + 1 < s1) take |= 0xffff0000u;
-                x[i] = (x[i] & take) | (y[i] & ~take);
-            }
-            *reinterpret_cast<u32x4 *>(tail + e * 8) = x;
-        }
+        for (int e = lane; e < HD * 4; e += 64) copy_slots(tail + e * 8, tile + e * 8, 8 * (e & 3), s0, s1);
     } else {
         const uint16_t *first = rows + (size_t)b1 * KVQ_BLOCK * HD;
         for (int e = s0 * HD / 8 + lane; e < s1 * HD / 8; e += 64)
@@ -262,8 +273,8 @@ template <bool F8, int HD> __global__ __launch_bounds__(256) void k_kvq_load(Loa
     }
     if (is_v) {
         const uint16_t *tail = a.c.v_tail + lh * KVQ_TAIL * HD;
-        for (int e = lane; e < HD * 32; e += 64)
-            if ((e & 31) < r) to[e] = tail[e];
+#pragma unroll
+        for (int e = lane; e < HD * 4; e += 64) copy_slots(to + e * 8, tail + e * 8, 8 * (e & 3), 0, r);
     } else {
         const uint16_t *tail = a.c.k_tail + lh * KVQ_TAIL * HD;
         for (int e = lane; e < r * HD / 8; e += 64)
@@ -272,75 +283,130 @@ template <bool F8, int HD> __global__ __launch_bounds__(256) void k_kvq_load(Loa
 }
 
 // ---------------------------------------------------------------------------
-// Advance: a workgroup per (layer, head) and K or V.  Logical row t of the new tail
-// is old slot src[t]; every row is in LDS before any is written.
+// Advance: a workgroup per (layer, head) and V or K.  New row j is accepted where bit j
+// of `mask` is set, and follows those below it, so a row's place is a count of bits.
+// Every row that is needed is in LDS, in its new order, before any is written.  A
+// block's hd / 32 KB are quantised by different waves, which share its maximum.
 
 struct AdvanceArgs {
     KvqLayers c;
+    uint64_t mask;
     int32_t total, full, first;  // rows, whole blocks among them, first row whose slot changes
-    int32_t src[KVQ_TAIL];
+    int32_t last;                // last accepted row's slot
 };
-
-template <bool F8, int HD> __global__ __launch_bounds__(256) void k_kvq_advance(AdvanceArgs a)
+// V in LDS: slots of a dim from the octet of the first needed row on, an odd number of
+// 16 bytes apart
+__host__ __device__ constexpr int advance_stride(int total, int lo) { return ((total - lo / 8 * 8 + 7) / 8 | 1) * 8; }
+__host__ __device__ constexpr int advance_lds(int hd, int total, int lo)  // 16-bit numbers
 {
-    __shared__ __align__(16) uint16_t buf[KVQ_TAIL * HD];
-    __shared__ int src[KVQ_TAIL];
+    return (total - lo) * hd > advance_stride(total, lo) * hd ? (total - lo) * hd : advance_stride(total, lo) * hd;
+}
+
+template <bool F8, int HD> __global__ __launch_bounds__(256, 6) void k_kvq_advance(AdvanceArgs a)
+{
+    constexpr int NJ = HD / 32, nt = 256;
+    extern __shared__ __align__(16) uint16_t buf[];
+    __shared__ uint32_t sm_top[2][NJ];
+    __shared__ __align__(8) uint8_t sm_row[KVQ_TAIL];  // the row that a slot becomes, 255: none
     const int64_t lh = blockIdx.x;
-    const bool is_v = blockIdx.y != 0;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n = lane & 15, g = lane >> 4;
+    const bool is_v = blockIdx.y == 0;  // (the longer ones first)
+    const int tid = threadIdx.x, lane = tid & 63, n = lane & 15, g = lane >> 4;
+    const int r = a.c.len % KVQ_BLOCK;
     uint16_t *tail = (is_v ? a.c.v_tail : a.c.k_tail) + lh * KVQ_TAIL * HD;
-    const int lo = a.full ? 0 : a.first;  // rows from here on are needed
-    if (tid < a.total) src[tid] = a.src[tid];
+    const int lo = a.full ? 0 : a.first, lo8 = lo / 8 * 8;  // rows from here on are needed
+    const int vs = advance_stride(a.total, lo);
+    if (tid < KVQ_TAIL) {
+        const uint64_t bit = 1ull << ((tid - r) & 63);
+        sm_row[tid] = tid < r ? tid : tid <= a.last && a.mask & bit ? r + __popcll(a.mask & (bit - 1)) : 255;
+    }
+    constexpr int IN = 3 * HD * 4 / nt;  // 16 bytes each of at most three tiles, all in flight
+    u32x4 x[IN];
+    auto slot = [&](int e) { return (lo / 32 + e / (HD * 4)) * 32 + 8 * (e & 3); };  // V: first of eight
     if (is_v) {
-        // the tiles from the first needed row's to the last source's, as they are
-        const int e1 = (a.src[a.total - 1] / 32 + 1) * HD * 4;
-        for (int e = lo / 32 * HD * 4 + tid; e < e1; e += 256)
-            *reinterpret_cast<u32x4 *>(buf + e * 8) = *reinterpret_cast<const u32x4 *>(tail + e * 8);
+        const int end = (a.last / 32 + 1 - lo / 32) * HD * 4;
+        auto skip = [&](int e) { return e >= end || slot(e) < lo8 || slot(e) > a.last; };
+#pragma unroll
+        for (int k = 0; k < IN; ++k) {
+            const int e = tid + k * nt, s = slot(e), d = e / 4 % HD;
+            if (!skip(e)) x[k] = *reinterpret_cast<const u32x4 *>(tail + ((s >> 5) * HD + d) * 32 + (s & 31));
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < IN; ++k) {
+            const int e = tid + k * nt;
+            if (skip(e)) continue;
+            const uint2 row = *reinterpret_cast<const uint2 *>(sm_row + slot(e));
+            uint16_t *to = buf + e / 4 % HD * vs - lo8;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t t = ((i < 4 ? row.x : row.y) >> (8 * (i & 3))) & 0xff;
+                if (t != 255) to[t] = (uint16_t)(x[k][i >> 1] >> (16 * (i & 1)));
+            }
+        }
     } else {
-        // rows in their new order
-        for (int e = lo * HD / 8 + tid; e < a.total * HD / 8; e += 256) {
-            const int t = e / (HD / 8), d = e % (HD / 8);
-            *reinterpret_cast<u32x4 *>(buf + e * 8) = *reinterpret_cast<const u32x4 *>(tail + a.src[t] * HD + d * 8);
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < IN; ++k) {
+            const int e = tid + k * nt, s = lo + e / (HD / 8);
+            if (s <= a.last && sm_row[s] != 255) x[k] = *reinterpret_cast<const u32x4 *>(tail + s * HD + e % (HD / 8) * 8);
+        }
+#pragma unroll
+        for (int k = 0; k < IN; ++k) {
+            const int e = tid + k * nt, s = lo + e / (HD / 8);
+            if (s <= a.last && sm_row[s] != 255) *reinterpret_cast<u32x4 *>(buf + (sm_row[s] - lo) * HD + e % (HD / 8) * 8) = x[k];
         }
     }
     __syncthreads();
-    // eight slots of a dim of V, in the new order
-    auto v8 = [&](int t, int d) {
-        u32x4 x;
+    if (a.full) {
+        // unit (block, KB), 4 waves: at most two each
+        constexpr int MOST = 2 * NJ / 4;
+        u32x4 x[MOST][2];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int s = src[t + 2 * i], s2 = src[t + 2 * i + 1];
-            x[i] = (uint32_t)buf[((s >> 5) * HD + d) * 32 + (s & 31)] | (uint32_t)buf[((s2 >> 5) * HD + d) * 32 + (s2 & 31)] << 16;
+        for (int k = 0; k < MOST; ++k) {
+            const int u = (tid >> 6) + 4 * k, b = u / NJ, j = u % NJ;
+            if (u >= a.full * NJ) break;
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+                x[k][half] = *reinterpret_cast<const u32x4 *>(
+                    is_v ? buf + (32 * j + 16 * half + n) * vs + b * KVQ_BLOCK + 8 * g
+                         : buf + (b * KVQ_BLOCK + k_slot(lane, j & 1)) * HD + 64 * (j >> 1) + 32 * half + 8 * g);
+            const uint32_t top = wave_max(max_bits(max_bits(0, x[k][0]), x[k][1]));
+            if (lane == 0) sm_top[b][j] = top;
         }
-        return x;
-    };
-    if (wave < a.full) {
-        const int64_t at = lh * a.c.nb + a.c.len / KVQ_BLOCK + wave;
-        uint8_t *codes = (is_v ? a.c.v : a.c.k) + at * KVQ_BLOCK * HD;
-        float *scale = a.c.scale + at * 2 + is_v;
-        if (is_v)
-            quantise<F8, HD>([&](int j, int half) { return v8(wave * KVQ_BLOCK + 8 * g, 32 * j + 16 * half + n); }, codes, scale,
-                             lane);
-        else
-            quantise<F8, HD>(
-                [&](int j, int half) {
-                    const int s = wave * KVQ_BLOCK + k_slot(lane, j & 1), d = 64 * (j >> 1) + 32 * half + 8 * g;
-                    return *reinterpret_cast<const u32x4 *>(buf + s * HD + d);
-                },
-                codes, scale, lane);
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < MOST; ++k) {
+            const int u = (tid >> 6) + 4 * k, b = u / NJ, j = u % NJ;
+            if (u >= a.full * NJ) break;
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < NJ; ++i) top = max(top, sm_top[b][i]);
+            const BlockScale s = block_scale<F8>(top);
+            const int64_t at = lh * a.c.nb + a.c.len / KVQ_BLOCK + b;
+            put_codes<F8>(x[k][0], x[k][1], s.inv, (is_v ? a.c.v : a.c.k) + at * KVQ_BLOCK * HD + (j * 64 + lane) * 16);
+            if (j == 0 && lane == 0) a.c.scale[at * 2 + is_v] = s.scale;
+        }
     }
-    // the rows behind the whole blocks, from the tail's start
-    const int base = a.full * KVQ_BLOCK, s0 = a.full ? 0 : a.first, s1 = a.total - base;
+    // the rows behind the whole blocks, from the tail's start; slots [s0, s1) change
+    const int base = a.full * KVQ_BLOCK, s0 = a.full ? 0 : lo8, s1 = a.total - base;
     if (is_v) {
-        for (int e = tid; e < HD * 32 * ((s1 + 31) / 32); e += 256) {
-            const int d = e / 32 % HD, s = e / (32 * HD) * 32 + e % 32;
+#pragma unroll
+        for (int k = 0; k < IN; ++k) {
+            const int e = tid + k * nt, s = slot(e), d = e / 4 % HD;
             if (s < s0 || s >= s1) continue;
-            const int o = src[base + s];
-            tail[e] = buf[((o >> 5) * HD + d) * 32 + (o & 31)];
+            // (slots behind the rows keep what the same thread read from them)
+            u32x4 y = *reinterpret_cast<const u32x4 *>(buf + d * vs + base + s - lo8);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t keep = (s + 2 * i < s1 ? 0u : 0xffffu) | (s + 2 * i + 1 < s1 ? 0u : 0xffff0000u);
+                y[i] = (y[i] & ~keep) | (x[k][i] & keep);
+            }
+            *reinterpret_cast<u32x4 *>(tail + ((s >> 5) * HD + d) * 32 + (s & 31)) = y;
         }
     } else {
-        for (int e = s0 * HD / 8 + tid; e < s1 * HD / 8; e += 256)
-            *reinterpret_cast<u32x4 *>(tail + e * 8) = *reinterpret_cast<const u32x4 *>(buf + base * HD + e * 8);
+        const int k0 = a.full ? 0 : lo;
+        for (int e = k0 * (HD / 8) + tid; e < s1 * (HD / 8); e += nt)
+            *reinterpret_cast<u32x4 *>(tail + e * 8) = *reinterpret_cast<const u32x4 *>(buf + (base - lo) * HD + e * 8);
     }
 }
 
@@ -945,7 +1011,8 @@ template <bool F8, int HD> hipError_t load(const LoadArgs &a, unsigned grid, hip
 }
 template <bool F8, int HD> hipError_t advance(const AdvanceArgs &a, hipStream_t s)
 {
-    hipLaunchKernelGGL((k_kvq_advance<F8, HD>), dim3((unsigned)(a.c.L * a.c.H), 2), dim3(256), 0, s, a);
+    const int lds = advance_lds(HD, a.total, a.full ? 0 : a.first) * 2;
+    hipLaunchKernelGGL((k_kvq_advance<F8, HD>), dim3((unsigned)(a.c.L * a.c.H), 2), dim3(256), lds, s, a);
     return hipGetLastError();
 }
 
@@ -988,10 +1055,11 @@ hipError_t launch_kvq_advance(const KvqLayers &c, const int32_t *path, int n, hi
     a.total = r + n;
     a.full = a.total / KVQ_BLOCK;
     a.first = a.total;
-    for (int t = 0; t < a.total; ++t) {
-        a.src[t] = t < r ? t : r + path[t - r];
-        if (a.src[t] != t && t < a.first) a.first = t;
+    for (int i = n - 1; i >= 0; --i) {
+        a.mask |= 1ull << path[i];
+        if (path[i] != i) a.first = r + i;
     }
+    a.last = r + path[n - 1];
     if (!a.full && a.first == a.total) return hipSuccess;  // every row stays where it is
     return KVQ_DISPATCH(c, advance, a, s);
 }
