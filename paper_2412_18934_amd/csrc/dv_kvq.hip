@@ -86,7 +86,7 @@ template <bool F8> __device__ __forceinline__ uint2 codes8(const u32x4 &x, float
 template <bool F8> __device__ __forceinline__ void put_codes(const u32x4 &x, const u32x4 &y, float inv, uint8_t *to)
 {
     const uint2 lo = codes8<F8>(x, inv), hi = codes8<F8>(y, inv);
-    *reinterpret_cast<u32x4 *>(to) = (u32x4){lo.x, lo.y, hi.x, hi.y};
+    __builtin_nontemporal_store((u32x4){lo.x, lo.y, hi.x, hi.y}, reinterpret_cast<u32x4 *>(to));
 }
 
 // Eight codes as bf16, exact: int8 has 8 significant bits, e4m3 four and exponents
@@ -195,7 +195,7 @@ template <bool F8, int HD> __global__ __launch_bounds__(256) void k_kvq_store(St
             quantise<F8, HD>(
                 [&](int j, int half) {
                     const int e = (32 * j + 16 * half + n) * 32 + 8 * g;
-                    u32x4 x = *reinterpret_cast<const u32x4 *>(tile + e);
+                    u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(tile + e));
                     if (8 * g < old) {
                         const u32x4 y = *reinterpret_cast<const u32x4 *>(tail + e);
 #pragma unroll
@@ -212,7 +212,7 @@ template <bool F8, int HD> __global__ __launch_bounds__(256) void k_kvq_store(St
                 [&](int j, int half) {
                     const int s = k_slot(lane, j & 1), d = 64 * (j >> 1) + 32 * half + 8 * g;
                     const uint16_t *p = s < old ? tail + s * HD : rows + (size_t)((b0 + job) * KVQ_BLOCK + s) * HD;
-                    return *reinterpret_cast<const u32x4 *>(p + d);
+                    return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p + d));
                 },
                 codes, scale, lane);
         }
@@ -259,7 +259,7 @@ template <bool F8, int HD> __global__ __launch_bounds__(256) void k_kvq_load(Loa
         const float scale = a.c.scale[at * 2 + is_v];
         u32x4 x[NJ];
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) x[j] = *reinterpret_cast<const u32x4 *>(codes + (j * 64 + lane) * 16);
+        for (int j = 0; j < NJ; ++j) x[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(codes + (j * 64 + lane) * 16));
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
@@ -267,7 +267,7 @@ template <bool F8, int HD> __global__ __launch_bounds__(256) void k_kvq_load(Loa
                 const u32x4 y = scaled_bf16(bf16_of<F8>(x[j][2 * half], x[j][2 * half + 1]), scale);
                 const int e = is_v ? (32 * j + 16 * half + n) * 32 + 8 * g
                                    : k_slot(lane, j & 1) * HD + 64 * (j >> 1) + 32 * half + 8 * g;
-                *reinterpret_cast<u32x4 *>(to + e) = y;
+                __builtin_nontemporal_store(y, reinterpret_cast<u32x4 *>(to + e));
             }
         return;
     }
