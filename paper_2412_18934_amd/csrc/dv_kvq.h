@@ -36,27 +36,35 @@ hipError_t launch_kvq_load(const KvqLayers &c, const KvqRows &to, hipStream_t s)
 // ones; blocks that are full become codes, the rest moves to the tail's start.
 hipError_t launch_kvq_advance(const KvqLayers &c, const int32_t *path, int n, hipStream_t s);
 
-// How a call's keys are cut: row tiles of up to 16 rt query rows (a KV head's
-// n x group rows), n_split ranges of per_split 32-key tiles each.
+// How a call's keys are cut: row tiles of up to 16 rt query rows (a KV head's n x
+// group rows) in z groups, n_split ranges of per_split 32-key tiles each.  A workgroup's
+// 8 waves take a tile each at a time, so z n_split heads is about the CUs.
+//
+// rt 2 reads and converts a tile once for 32 rows, rt 1 has twice the workgroups and no
+// waiting for the longer sums: 1 up to 12 tiles a wave.  us by tiles a wave, rt 1 / 2: 2.0
+// (8 heads x 32 rows, 8192 slots) 12.5 / 15.6, 5.2 (40 x 60, 2077) 16.0 / 18.2, 8.0 (8 x 64,
+// 16384) 19.6 / 21.4, 16 (32 x 32, 16384) 34.5 / 32.5, 32 (8 x 32, 130001) 64 / 59.
+//
+// Ranges of less than 8 tiles leave waves idle, and several ranges cost a second launch,
+// so up to 24 tiles stay one: 17 tiles of 32 heads 7.8 us as one range, 8.5 as three; 22 of 8
+// heads 8.7 and 8.6; 34 of 40 heads 10.5 and 9.9; 32 of 8 heads 10.3 and 8.5.
 struct KvqCut {
     int rt, z, per_split, n_split;
 };
-inline int kvq_row_tiles(int rows) { return rows <= 16 ? 1 : 2; }
-inline int kvq_row_groups(int rows) { return (rows + 16 * kvq_row_tiles(rows) - 1) / (16 * kvq_row_tiles(rows)); }
-// the most ranges of any cache length: about one workgroup per CU
+inline int kvq_row_groups(int rows, int rt) { return (rows + 16 * rt - 1) / (16 * rt); }
+// the most ranges of any cache length
 inline int kvq_max_split(int heads, int rows, int n_cu)
 {
-    const int most = n_cu / (heads * kvq_row_groups(rows));
+    const int most = n_cu / (heads * kvq_row_groups(rows, 2));
     return most > 1 ? most : 1;
 }
 inline KvqCut kvq_cut(int heads, int rows, int tiles, int n_cu)
 {
     KvqCut c;
-    c.rt = kvq_row_tiles(rows);
-    c.z = kvq_row_groups(rows);
-    const int most = kvq_max_split(heads, rows, n_cu);
-    c.per_split = (tiles + most - 1) / most;
-    if (c.per_split < 8) c.per_split = 8;  // a tile for each wave
+    c.rt = (double)tiles * heads * kvq_row_groups(rows, 1) > 12. * 8 * n_cu && rows > 16 ? 2 : 1;
+    c.z = kvq_row_groups(rows, c.rt);
+    const int most = tiles <= 24 ? 1 : n_cu / (heads * c.z) > 1 ? n_cu / (heads * c.z) : 1;
+    c.per_split = (tiles + most - 1) / most > 8 ? (tiles + most - 1) / most : 8;
     c.n_split = (tiles + c.per_split - 1) / c.per_split;
     return c;
 }
