@@ -15,6 +15,8 @@ bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) %
 
 // A grid's work-items are counted in 32 bits: 2^24 workgroups of 256.
 constexpr int64_t MAX_GROUPS = (1ll << 24) - 1;
+// Query heads of a KV head: 64 rows each, 16 to a row group, are a grid's z (65535 at most).
+constexpr int MAX_GROUP = 1024;
 
 int check_kvq(dv_handle *h, const dv_kvq *c)
 {
@@ -245,8 +247,9 @@ int64_t dv_kvq_attention_workspace(const dv_kvq *c, int32_t n, int32_t n_heads)
     const int rc = check_kvq(nullptr, c);
     if (rc) return rc;
     if (n < 1 || n > KVQ_MAX_NEW) return set_err(nullptr, DV_EINVAL, "n %d outside [1, %d]", n, KVQ_MAX_NEW);
-    if (n_heads < 1 || n_heads > 65535 || n_heads % c->n_heads)
-        return set_err(nullptr, DV_EINVAL, "%d query heads do not share %d KV heads evenly", n_heads, c->n_heads);
+    if (n_heads < 1 || n_heads > 65535 || n_heads % c->n_heads || n_heads / c->n_heads > MAX_GROUP)
+        return set_err(nullptr, DV_EINVAL, "%d query heads do not share %d KV heads evenly, %d each at most", n_heads, c->n_heads,
+                       MAX_GROUP);
     int n_cu = 0;
     const hipError_t e = current_cus(&n_cu);
     if (e != hipSuccess) return set_err(nullptr, DV_EHIP, "compute units: %s", hipGetErrorString(e));
@@ -264,8 +267,9 @@ int dv_kvq_attention(const dv_kvq *c, int32_t layer, const float *q, int64_t q_s
     if (layer < 0 || layer >= c->n_layers) return set_err(nullptr, DV_EINVAL, "layer %d outside [0, %d)", layer, c->n_layers);
     if (!q || !out) return set_err(nullptr, DV_EINVAL, "null queries or output");
     if (n < 1 || n > KVQ_MAX_NEW) return set_err(nullptr, DV_EINVAL, "n %d outside [1, %d]", n, KVQ_MAX_NEW);
-    if (n_heads < 1 || n_heads > 65535 || n_heads % c->n_heads)
-        return set_err(nullptr, DV_EINVAL, "%d query heads do not share %d KV heads evenly", n_heads, c->n_heads);
+    if (n_heads < 1 || n_heads > 65535 || n_heads % c->n_heads || n_heads / c->n_heads > MAX_GROUP)
+        return set_err(nullptr, DV_EINVAL, "%d query heads do not share %d KV heads evenly, %d each at most", n_heads, c->n_heads,
+                       MAX_GROUP);
     const int64_t row = (int64_t)n_heads * c->head_dim;
     if (!aligned(q, 16) || !aligned(out, 16) || q_stride < row || out_stride < row || q_stride % 4 || out_stride % 4 ||
         q_stride > (1ll << 40) || out_stride > (1ll << 40))

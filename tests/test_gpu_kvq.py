@@ -344,6 +344,41 @@ def test_attention(fmt, hd, len0, n, heads, group, kind):
         assert not got[::3].any()                     # rows that see nothing
 
 
+@pytest.mark.parametrize("fmt,hd", [("i8", 64), ("f8", 64), ("i8", 128), ("f8", 128)])
+def test_attention_of_many_rows_over_a_long_cache(fmt, hd):
+    """32 rows a workgroup (more than 12 tiles a wave), random codes."""
+    rng = np.random.default_rng(18)
+    heads, n, length = 16, 61, 14005
+    g = D.DeviceKVQ(1, heads, hd, 14112, fmt)
+    for t in (g.k, g.v):
+        codes = rng.integers(-127, 128, t.shape, dtype=np.int8) if fmt == "i8" else ok.e4m3_code(
+            rng.normal(0, 100, t.shape).clip(-448, 448)).view(np.int8)
+        t.copy_(torch.from_numpy(codes))
+    g.scale.copy_(torch.from_numpy(np.exp(rng.normal(-4 if fmt == "i8" else -5, 0.7, g.scale.shape))))
+    g.k_tail.normal_()
+    g.v_tail.normal_()
+    g.c.len = length
+    q = rng.normal(0, 1.4, (n, heads, hd)).astype(np.float32)
+    mask, sees = _sees(rng, n, "tree")
+    qd = torch.from_numpy(q).to(DEV)
+    ws = torch.full((dv.dv_kvq_attention_workspace(g.c, n, heads) // 4,), float("nan"), device=DEV)
+    dv.dv_kvq_attention(g.c, 0, qd.data_ptr(), heads * hd, n, heads, mask, qd.data_ptr(), heads * hd, ws.data_ptr(), ws.nbytes)
+    torch.cuda.synchronize()
+    got = qd.double().cpu().numpy()                   # (out may be q)
+    k, v = _oracle_kv(g, 1, heads)[0]
+    every = np.concatenate([np.ones((n, length), bool), sees], axis=1)
+    r = length % 32
+    for h in (0, 7, 15):
+        kh = np.concatenate([k[h], g.k_tail[0, h, r:r + n].double().cpu().numpy()])
+        vt = g.v_tail[0, h].transpose(1, 2).reshape(96, hd)
+        vh = np.concatenate([v[h], vt[r:r + n].double().cpu().numpy()])
+        qh = q[:, h].astype(np.float64)
+        want = ok.attention(qh, kh, vh, every)
+        err, tol = np.abs(got[:, h] - want), _tolerance(qh, kh, vh, every)[:, None]
+        assert (err <= tol).all(), "head %d: %g" % (h, err.max())
+        print("[kvq] %s hd %d head %d: worst error %.2g" % (fmt, hd, h, err.max()), flush=True)
+
+
 @pytest.mark.parametrize("fmt", ["i8", "f8"])
 def test_attention_strides_and_layers(fmt):
     rng = np.random.default_rng(11)

@@ -87,7 +87,7 @@ def test_advance_refusals(path):
     (dict(layer=-1), -1), (dict(layer=2), -1), (dict(q=0), -1), (dict(out=0), -1), (dict(n=0), -1), (dict(n=65), -1),
     (dict(n_heads=0), -1), (dict(n_heads=6), -1), (dict(n_heads=65540), -1), (dict(q=A + 4), -1), (dict(out=A + 8), -1),
     (dict(q_stride=255), -1), (dict(q_stride=258), -1), (dict(out_stride=-256), -1), (dict(out_stride=1 << 50), -1),
-    (dict(n_heads=8), -1), (dict(len=250, n=7), dv.DV_ECAPACITY)])
+    (dict(n_heads=8), -1), (dict(n_heads=4100, q_stride=4100 * 64, out_stride=4100 * 64), -1), (dict(len=250, n=7), dv.DV_ECAPACITY)])
 def test_attention_refusals(kw, code):
     a = dict(layer=1, q=A, q_stride=256, n=4, n_heads=4, out=A, out_stride=256, len=40)
     a.update(kw)
