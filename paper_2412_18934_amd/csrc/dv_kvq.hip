@@ -707,18 +707,21 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
         m_run[rt] = mnew;
     };
 
+    // the unit of the sums at least u
+    auto grow = [&](float u) {
+        if (!(u > v_unit)) return;
+        const float r = v_unit / u;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[rt][dt][j] *= r;
+        v_unit = u;
+        v_inv = 1.f / u;
+    };
     auto codes = [&](const Raw &x) {
-        if (x.s.y > v_unit) {
-            const float r = v_unit / x.s.y;
-#pragma unroll
-            for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) o[rt][dt][j] *= r;
-            v_unit = x.s.y;
-            v_inv = 1.f / x.s.y;
-        }
+        grow(x.s.y);
         const float vs = x.s.y * v_inv * W_UNIT;
         u32x4 v[ND];
 #pragma unroll
@@ -828,7 +831,8 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
                     if ((v[dt][w] & 0x7f80u) == 0x7f80u) v[dt][w] &= 0xffff0000u;
                     if ((v[dt][w] & 0x7f800000u) == 0x7f800000u) v[dt][w] &= 0xffffu;
                 }
-        if (v_unit == 0.f) v_unit = v_inv = 1.f;  // no sums yet, or only zeros
+        // the sums' unit holds these numbers too (2^64: up to 2^128 they stay far from fp32's end)
+        grow(__any((top & 0xffffu) >= 0x5f80u || top >= 0x5f800000u) ? 0x1p64f : 1.f);
         const float vs = v_inv * W_UNIT;
         each<RT>([&](auto rt_) {
             constexpr int rt = decltype(rt_)::value;

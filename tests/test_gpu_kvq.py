@@ -433,6 +433,21 @@ def test_large_scores():
         _check_attention(p, rng, 6, 1, "tree", q=rng.normal(0, size, (6, 2, 64)).astype(np.float32).astype(np.float64))
 
 
+def test_values_of_any_size():
+    """Tiny and huge values side by side: nothing overflows on the way."""
+    rng = np.random.default_rng(19)
+    for fmt in ("i8", "f8"):
+        for old, new in ((2.0 ** -97, 300.0), (2.0 ** -97, 2.0 ** 118), (2.0 ** 110, 2.0 ** -60), (2.0 ** 118, 2.0 ** 118), (0.0, 1.0)):
+            p = Pair(1, 2, 64, 192, fmt)
+            rows = {"k": _rows(rng, (1, 2, 70, 64)), "v": ov.round_to_bf16(rng.normal(0, 1, (1, 2, 70, 64)) * old)}
+            kv = _kv(p, 192, rows)
+            dv.dv_kvq_store(p.g.c, kv.c, 70)
+            p.append(rows)
+            fresh = {"k": _rows(rng, (1, 2, 5, 64)), "v": ov.round_to_bf16(rng.normal(0, 1, (1, 2, 5, 64)) * new)}
+            got, _ = _check_attention(p, rng, 5, 1, "tree", new=fresh)
+            assert np.isfinite(got).all()
+
+
 def test_offsets_past_32_bits():
     """The last layer and head of a cache whose codes and tail lie beyond 4 GiB."""
     nl, nh, hd, cap, n = 9, 64, 128, 65536, 3
