@@ -376,7 +376,8 @@ int dv_kvq_advance(dv_kvq *kvq, const int32_t *path, int32_t n, void *stream);
  *   q, out: device fp32 [n][n_heads][head_dim], rows q_stride and out_stride floats
  *     apart (multiples of 4, at least n_heads head_dim), 16-byte aligned.  n_heads is
  *     a multiple of kvq->n_heads, at most 1024 times as many: query heads h with the
- *     same h / (n_heads / kvq->n_heads) share a KV head.  out may be q;
+ *     same h / (n_heads / kvq->n_heads) share a KV head.  out may be q, with
+ *     the same stride; they may not overlap otherwise;
  *   mask: HOST array of n;
  *   workspace: device memory, 16-byte aligned, of at least
  *     dv_kvq_attention_workspace(kvq, n, n_heads) bytes (enough for any len of this

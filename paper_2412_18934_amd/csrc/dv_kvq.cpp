@@ -274,6 +274,9 @@ int dv_kvq_attention(const dv_kvq *c, int32_t layer, const float *q, int64_t q_s
     if (!aligned(q, 16) || !aligned(out, 16) || q_stride < row || out_stride < row || q_stride % 4 || out_stride % 4 ||
         q_stride > (1ll << 40) || out_stride > (1ll << 40))
         return set_err(nullptr, DV_EINVAL, "queries and outputs need 16-byte aligned rows of at least %lld floats", (long long)row);
+    // (another row's output would be written over queries that are still to be read)
+    if (q == out && n > 1 && q_stride != out_stride)
+        return set_err(nullptr, DV_EINVAL, "outputs in place of the queries need their row stride");
     if ((int64_t)c->len + n > c->capacity)
         return set_err(nullptr, DV_ECAPACITY, "len %d + %d exceeds the 8-bit cache's capacity %d", c->len, n, c->capacity);
     int n_cu = 0;

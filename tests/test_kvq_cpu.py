@@ -101,6 +101,12 @@ def test_attention_refusals(kw, code):
                 dv.dv_kvq_attention_workspace(cache(), a["n"], a["n_heads"])
 
 
+def test_attention_in_place_needs_one_stride():
+    with pytest.raises(dv.DvError) as e:
+        dv.dv_kvq_attention(cache(), 1, A, 512, 4, 4, None, A, 256, A, 1 << 40)
+    assert e.value.code == dv.DV_EINVAL and "stride" in str(e.value)
+
+
 def test_handle_calls_refuse_a_null_handle():
     acc = dv.dv_accept()
     for call in (lambda: dv.dv_verify_step_kvq(None, [0], [-1], cache()), lambda: dv.dv_prefill_kvq(None, [0], cache()),
