@@ -165,7 +165,15 @@ __device__ __forceinline__ void copy_slots(uint16_t *to, const uint16_t *from, i
 // ---------------------------------------------------------------------------
 // Store: a wave per block and per K or V (blockIdx.y), four to a workgroup.  The
 // wave of a head's first block also writes the new tail, after it has read the old
-// one (both by the same wave, in that order).  Moves 3 bytes per number.
+// one (both by the same wave, in that order).
+//
+// A block is a wave's registers: 16 bytes per lane and load, one maximum over the
+// wave, 16 bytes of codes per lane and store, in the operands' order.  So nothing goes
+// through LDS and the rows are read once.  Bound by memory: 2 bytes read and 1 written
+// per number, none of them used again here, so they go past the caches (1024 rows of a
+// 13B model's 1600 heads, 1.26 GB: 206 us, 6.1 TB/s; through them 220).  150 rows of 1024
+// heads (129 MB) take 32.5 us (37.5), 4.0 TB/s: a wave has one block, which is loaded,
+// reduced and stored with nothing else in flight; few rows take a launch, 3.7 us.
 
 struct StoreArgs {
     KvqLayers c;
@@ -233,7 +241,13 @@ template <bool F8, int HD> __global__ __launch_bounds__(256) void k_kvq_store(St
 }
 
 // ---------------------------------------------------------------------------
-// Load: a wave per block, the tail's committed rows as one more.
+// Load: a wave per block, the tail's committed rows as one more; store backwards, 1 byte
+// read and 2 written per number.  Bound by memory: 8191 slots of 320 heads (2.0 GB)
+// 393 us, 5.1 TB/s; 333 slots of 1024 heads (265 MB) 54.5 us, 4.9 TB/s, and through the
+// caches 61.
+//
+// A number is its code x scale, rounded to fp32 and then to bf16, the cache's type: two
+// roundings of 2^-24 and 2^-8, beside a code's own of up to half a step.
 
 struct LoadArgs {
     KvqLayers c;
@@ -287,6 +301,13 @@ template <bool F8, int HD> __global__ __launch_bounds__(256) void k_kvq_load(Loa
 // of `mask` is set, and follows those below it, so a row's place is a count of bits.
 // Every row that is needed is in LDS, in its new order, before any is written.  A
 // block's hd / 32 KB are quantised by different waves, which share its maximum.
+//
+// Moves a few KB per head, so it is bound by the latency of one read, LDS and write
+// chain: all loads of a thread are in flight at once, V is written in whole octets of
+// slots, and 6 workgroups share a CU, so that the 3200 of a 13B model are about two
+// rounds.  5 of 16 rows of its 1600 heads (8.2 MB) 8.2 us; 38 of 64 rows of 1024 heads,
+// two blocks filled (52 MB), 14.7 us, 3.6 TB/s.  A wave for each block of a head and one
+// for the rest took 16 us.
 
 struct AdvanceArgs {
     KvqLayers c;
@@ -441,6 +462,26 @@ template <bool F8, int HD> __global__ __launch_bounds__(256, 6) void k_kvq_advan
 // above it, which after the first tiles is rare.  V's scales likewise: the sums are
 // in units of the largest scale so far.  So a weight is at most 2^(LAZY + 11) = 2^15 in
 // fp16, which holds 65504.
+//
+// Roundings: a query to 2^-23 of its row's largest (int8) or 2^-22 of itself (e4m3), a
+// weight to 2^-22 of itself or 2^-35 of the largest a row can have; products and sums are
+// fp32 (int8 scores integers).  Against 64 bits the outputs are about as near as a
+// plain fp32 computation's.
+//
+// What bounds it: with few rows the codes' bytes (2 hd + 8 / 32 per key and head); with
+// more, the conversion of V and the parts' matrix instructions, which come per tile and
+// per row.  8 waves of a workgroup take tiles of their own, so no barrier stands between
+// tiles, and each keeps two tiles (16 KB) in flight, 128 KB per CU.  Times,
+// with the merge where there is one:
+//   8 heads x 32 rows, 130001 slots (267 MB)    58 us, 4.6 TB/s: the stream (its loads
+//                                               alone take 52)
+//   32 heads x 1 row, 8191 slots (67 MB)        17.9 us: start, 4 tiles a wave, merge
+//   40 heads x 60 rows, 2077 slots, e4m3        16.1 us: 160 workgroups, 9 tiles a wave
+//   40 heads x 16 rows, 1037 slots (12 MB)       9.9 us: latencies of 1 tile a wave, merge
+// Measured and not taken: 4 waves a workgroup (1 to 6 per CU), 16 waves per CU, a
+// single buffer and 128 registers (spills), 64 rows a workgroup, workgroups of a head
+// on one XCD, a higher wave priority at the matrix instructions, more independent
+// chains of them: each equal or slower.
 
 constexpr float LAZY = 4.f, W_UNIT = 2048.f;
 
@@ -942,7 +983,11 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
 }
 
 // The ranges combined, in a launch of its own: 4 threads share a row's 4 dims, each with
-// every fourth range, and are combined in LDS.
+// every fourth range, and are combined in LDS.  The order is fixed, so are the results.
+// 3.4 to 4.7 us, a launch and three dependent reads.  The last workgroup of a head
+// doing it in place of a launch was slower everywhere: it waits for its own writes and
+// for a counter, then merges alone (32 heads x 1 row, 8191 slots 18.7 us for 17.9; 8 x 32,
+// 130001 slots 67 for 58).
 template <int HD> __global__ __launch_bounds__(256) void k_kvq_merge(KvqOut a)
 {
     constexpr int D4 = HD / 4, NR = 64 / D4;  // rows of a workgroup
