@@ -142,7 +142,7 @@ def lib():
         L.dv_kvq_store.restype = ctypes.c_int
         L.dv_kvq_load.argtypes = [kvqp, ctypes.POINTER(dv_kv), vp]
         L.dv_kvq_load.restype = ctypes.c_int
-        L.dv_kvq_advance.argtypes = [kvqp, i32p, i32, vp]
+        L.dv_kvq_advance.argtypes = [kvqp, vp, i32, vp]
         L.dv_kvq_advance.restype = ctypes.c_int
         L.dv_kvq_attention.argtypes = [kvqp, i32, vp, i64, i32, i32, vp, vp, i64, vp, i64, vp]
         L.dv_kvq_attention.restype = ctypes.c_int
@@ -301,7 +301,7 @@ def dv_kvq_load(kvq: dv_kvq, kv: dv_kv, stream: int = 0):
 def dv_kvq_advance(kvq: dv_kvq, path, stream: int = 0):
     """path: host array of new rows, increasing."""
     p = _i32(path)
-    _check(lib().dv_kvq_advance(kvq, _ptr(p), len(p), stream or None), None)
+    _check(lib().dv_kvq_advance(kvq, p.tobytes(), len(p), stream or None), None)  # (bytes: a pointer at least cost)
 
 
 def dv_kvq_attention_workspace(kvq: dv_kvq, n: int, n_heads: int) -> int:
@@ -318,10 +318,10 @@ def dv_kvq_attention(kvq: dv_kvq, layer: int, q: int, q_stride: int, n: int, n_h
     n uint64, or None (row i sees new rows 0..i)."""
     at = None
     if mask is not None:
-        mask = np.ascontiguousarray(mask, dtype=np.uint64)
+        mask = np.asarray(mask, dtype=np.uint64)
         if len(mask) < n:
             raise ValueError("mask needs one entry per row")
-        at = mask.__array_interface__["data"][0]
+        at = mask.tobytes()
     _check(lib().dv_kvq_attention(kvq, layer, q or None, q_stride, n, n_heads, at, out or None, out_stride,
                                   workspace or None, workspace_bytes, stream or None), None)
 
