@@ -42,12 +42,12 @@ hipError_t launch_kvq_advance(const KvqLayers &c, const int32_t *path, int n, hi
 //
 // rt 2 reads and converts a tile once for 32 rows, rt 1 has twice the workgroups and no
 // waiting for the longer sums: 1 up to 12 tiles a wave.  us by tiles a wave, rt 1 / 2: 2.0
-// (8 heads x 32 rows, 8192 slots) 12.5 / 15.6, 5.2 (40 x 60, 2077) 16.0 / 18.2, 8.0 (8 x 64,
-// 16384) 19.6 / 21.4, 16 (32 x 32, 16384) 34.5 / 32.5, 32 (8 x 32, 130001) 64 / 59.
+// (8 heads x 32 rows, 8192 slots) 11.5 / 15.5, 5.2 (40 x 60, 2077) 15.1 / 18.1, 8.0 (8 x 64,
+// 16384) 18.6 / 20.5, 16 (32 x 32, 16384) 32.1 / 30.1, 32 (8 x 32, 130001) 58 / 55.
 //
 // Ranges of less than 8 tiles leave waves idle, and several ranges cost a second launch,
-// so up to 24 tiles stay one: 17 tiles of 32 heads 7.8 us as one range, 8.5 as three; 22 of 8
-// heads 8.7 and 8.6; 34 of 40 heads 10.5 and 9.9; 32 of 8 heads 10.3 and 8.5.
+// so up to 24 tiles stay one: 17 tiles of 32 heads 7.6 us as one range, 8.7 as three; 22 of 8
+// heads 8.8 and 8.7; 34 of 40 heads 10.3 and 10.0; 32 of 8 heads 9.9 and 8.6.
 struct KvqCut {
     int rt, z, per_split, n_split;
 };

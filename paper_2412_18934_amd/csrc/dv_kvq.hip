@@ -471,17 +471,19 @@ template <bool F8, int HD> __global__ __launch_bounds__(256, 6) void k_kvq_advan
 // What bounds it: with few rows the codes' bytes (2 hd + 8 / 32 per key and head); with
 // more, the conversion of V and the parts' matrix instructions, which come per tile and
 // per row.  8 waves of a workgroup take tiles of their own, so no barrier stands between
-// tiles, and each keeps two tiles (16 KB) in flight, 128 KB per CU.  Times,
-// with the merge where there is one:
-//   8 heads x 32 rows, 130001 slots (267 MB)    58 us, 4.6 TB/s: the stream (its loads
-//                                               alone take 52)
-//   32 heads x 1 row, 8191 slots (67 MB)        17.9 us: start, 4 tiles a wave, merge
-//   40 heads x 60 rows, 2077 slots, e4m3        16.1 us: 160 workgroups, 9 tiles a wave
-//   40 heads x 16 rows, 1037 slots (12 MB)       9.9 us: latencies of 1 tile a wave, merge
-// Measured and not taken: 4 waves a workgroup (1 to 6 per CU), 16 waves per CU, a
-// single buffer and 128 registers (spills), 64 rows a workgroup, workgroups of a head
-// on one XCD, a higher wave priority at the matrix instructions, more independent
-// chains of them: each equal or slower.
+// tiles, and each asks for its next tile when the scores of the last row tile have used
+// K (V is converted by then): 64 KB per CU in flight while weights and sums are made.
+// Times, with the merge where there is one, and with two tiles in flight in two sets of
+// registers, which is twice the code and no faster but for a single tile a wave:
+//   8 heads x 32 rows, 130001 slots (267 MB)  55.5 us (58.4), 4.8 TB/s; reading alone,
+//                                             this way cut, 45, and the merge 4
+//   32 heads x 1 row, 8191 slots (67 MB)      17.6 (18.1): reading alone 12.4, merge
+//   40 heads x 60 rows, 2077 slots, e4m3      15.0 (16.0): 160 workgroups, 9 tiles a wave
+//   40 heads x 16 rows, 1037 slots (12 MB)    10.0 (9.9): latencies of 1 tile a wave, merge
+// Measured and not taken: 4 waves a workgroup (1 to 6 per CU), 12 and 16 waves per CU
+// (spills), 64 rows a workgroup, workgroups of a head on one XCD, a higher wave priority
+// at the matrix instructions, more independent chains of them, V asked for before the
+// scores: each equal or slower.
 
 constexpr float LAZY = 4.f, W_UNIT = 2048.f;
 
@@ -604,12 +606,12 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
 
     struct Raw {
         u32x4 k[NC], v[NC];
-        float2 s;
+        float s;  // K's scale in even lanes, V's in odd ones
     };
     auto load = [&](int t, Raw &x) {
         const int64_t at = (int64_t)h * a.nb + t;
         const uint8_t *kp = a.k + at * KVQ_BLOCK * HD + lane * 16, *vp = a.v + at * KVQ_BLOCK * HD + lane * 16;
-        x.s = *reinterpret_cast<const float2 *>(a.scale + at * 2);
+        x.s = a.scale[at * 2 + (lane & 1)];
 #pragma unroll
         for (int j = 0; j < NC; ++j) x.k[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(kp + j * 1024));
 #pragma unroll
@@ -617,7 +619,7 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
     };
     const int t0 = split * a.per_split, t1 = min(a.tiles, t0 + a.per_split), c1 = min(t1, a.blocks);
     const bool has_tail = t1 > a.blocks;
-    Raw buf0, buf1;
+    Raw buf0, buf1;  // (buf1: a tail tile's other half, which is twice a tile of codes)
 
     // 8 dims of one row per thread; a row's threads are neighbours.  (Loads return in
     // order: the queries' go ahead of the first tile's.)
@@ -660,7 +662,7 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
         const int64_t at = (int64_t)h * a.nb + (tail_first ? 0 : t0 + wave);
         const char *kc = reinterpret_cast<const char *>(a.k + at * KVQ_BLOCK * HD + lane * 16);
         const char *vc = reinterpret_cast<const char *>(a.v + at * KVQ_BLOCK * HD + lane * 16);
-        buf0.s = *reinterpret_cast<const float2 *>(a.scale + at * 2);
+        buf0.s = a.scale[at * 2 + (lane & 1)];
         fetch(tail_first ? k0 : kc, tail_first ? 64 : 1024, tail_first ? v0 : vc, buf0);
     }
     if (qrow < RT * 16) {
@@ -707,7 +709,6 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
             for (int p = 0; p < 3; ++p) qt[row / 16][(c * 3 + p) * 64 + at] = t[p];
         }
     }
-    if (t0 + wave + NW < c1) load(t0 + wave + NW, buf1);
     if (tail_first && t0 + wave < t1) {
         const char *k0, *k1, *v0;
         tail_at(t0 + wave, k0, k1, v0);
@@ -761,9 +762,12 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
         v_unit = u;
         v_inv = 1.f / u;
     };
-    auto codes = [&](const Raw &x) {
-        grow(x.s.y);
-        const float vs = x.s.y * v_inv * W_UNIT;
+    // one tile, whose registers take tile `next` as soon as they are free
+    auto codes = [&](Raw &x, int next) {
+        const float k_scale = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x.s), 0));
+        const float v_scale = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x.s), 1));
+        grow(v_scale);
+        const float vs = v_scale * v_inv * W_UNIT;
         u32x4 v[ND];
 #pragma unroll
         for (int j = 0; j < NC; ++j)
@@ -780,7 +784,10 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
                 }
         each<RT>([&](auto rt_) {
             constexpr int rt = decltype(rt_)::value;
-            if (row0 + 16 * rt >= rows) return;
+            if (RT > 1 && row0 + 16 * rt >= rows) {
+                if (rt == RT - 1 && next < c1) load(next, x);
+                return;
+            }
             float s[8];
             if constexpr (F8) {
                 f32x4 sa = (f32x4){0.f, 0.f, 0.f, 0.f}, sb = sa;
@@ -809,7 +816,8 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
                     s[4 + i] = fmaf((float)sb[2][i], 65536.f, (float)(sb[1][i] * 256 + sb[0][i]));
                 }
             }
-            const float c = coef[rt] * x.s.x;
+            if (rt == RT - 1 && next < c1) load(next, x);
+            const float c = coef[rt] * k_scale;
             float mt = s[0];
 #pragma unroll
             for (int i = 1; i < 8; ++i) mt = fmaxf(mt, s[i]);
@@ -832,14 +840,7 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
             }
         });
     };
-    // two buffers in turn: a tile loads while the other is used
-    for (int t = t0 + wave; t < c1; t += 2 * NW) {
-        codes(buf0);
-        if (t + 2 * NW < c1) load(t + 2 * NW, buf0);
-        if (t + NW >= c1) break;
-        codes(buf1);
-        if (t + 3 * NW < c1) load(t + 3 * NW, buf1);
-    }
+    for (int t = t0 + __builtin_amdgcn_readfirstlane(wave); t < c1; t += NW) codes(buf0, t + NW);
 
     // tail tiles of the range, by the waves whose turn it is
     const int tt = max(t0, a.blocks);
