@@ -89,32 +89,23 @@ template <bool F8> __device__ __forceinline__ void put_codes(const u32x4 &x, con
     __builtin_nontemporal_store((u32x4){lo.x, lo.y, hi.x, hi.y}, reinterpret_cast<u32x4 *>(to));
 }
 
-// Eight codes as bf16, exact: int8 has 8 significant bits, e4m3 four and exponents
-// of -9 to 8.
-template <bool F8> __device__ __forceinline__ u32x4 bf16_of(uint32_t lo, uint32_t hi)
-{
-    u32x4 r;
-    if constexpr (F8) {
-        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-        r[0] = __builtin_bit_cast(uint32_t, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false));
-        r[1] = __builtin_bit_cast(uint32_t, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true));
-        r[2] = __builtin_bit_cast(uint32_t, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, false));
-        r[3] = __builtin_bit_cast(uint32_t, (bf16x2)__builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.f, true));
-    } else {
-        const uint2 a = i8x4_to_bf16(lo), b = i8x4_to_bf16(hi);
-        r = (u32x4){a.x, a.y, b.x, b.y};
-    }
-    return r;
-}
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
-// scale x code rounded to fp32, then to bf16
-__device__ __forceinline__ u32x4 scaled_bf16(const u32x4 &codes, float scale)
+// scale x code of eight codes, rounded to fp32, then to bf16 (nearest even)
+template <bool F8> __device__ __forceinline__ u32x4 scaled_bf16(uint32_t lo, uint32_t hi, float scale)
 {
     u32x4 r;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float lo = __uint_as_float(codes[i] << 16) * scale, hi = __uint_as_float(codes[i] & 0xffff0000u) * scale;
-        r[i] = (uint32_t)f2bf(lo) | (uint32_t)f2bf(hi) << 16;
+        const uint32_t w = i < 2 ? lo : hi;
+        f32x2 x;
+        if constexpr (F8)
+            x = i & 1 ? __builtin_amdgcn_cvt_pk_f32_fp8(w, true) : __builtin_amdgcn_cvt_pk_f32_fp8(w, false);
+        else
+            x = (f32x2){(float)(int8_t)(w >> (16 * (i & 1))), (float)(int8_t)(w >> (16 * (i & 1) + 8))};
+        const f32x2 y = {x[0] * scale, x[1] * scale};
+        r[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(y, bf16x2));
     }
     return r;
 }
@@ -123,18 +114,31 @@ __device__ __forceinline__ u32x4 scaled_bf16(const u32x4 &codes, float scale)
 // the two halves of the lane's 16 bytes in the block's j-th KB.
 __device__ __forceinline__ int k_slot(int lane, int t) { return 8 * ((lane & 15) >> 2) + 4 * t + (lane & 3); }
 
-// Quantise one block by one wave; get(j, half) gives eight bf16 numbers.
-template <bool F8, int HD, typename Get>
-__device__ __forceinline__ void quantise(Get get, uint8_t *codes, float *scale, int lane)
+// A lane's K numbers are two 64-byte pieces of its row.  For loads and stores of whole
+// 128-byte lines, lanes n and n ^ 8 exchange: the first halves of both rows become lane
+// n < 8's and the second ones lane n + 8's.  (Its own inverse.)
+__device__ __forceinline__ void swap_halves(u32x4 &x0, u32x4 &x1, bool upper)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t give = upper ? x0[i] : x1[i];
+        const uint32_t get = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)give, 0x128 /* rotate 16 lanes by 8 */, 0xf, 0xf, false);
+        if (upper) x0[i] = get;
+        else x1[i] = get;
+    }
+}
+// Where piece `half` of KB j is then: row n & 7 (half 0) or that + 8, its dims by the lane.
+__device__ __forceinline__ int k_line(int lane, int j, int half, int hd)
+{
+    return k_slot((lane & 55) | 8 * half, j & 1) * hd + 64 * (j >> 1) + 4 * (lane & 8) + 8 * (lane >> 4);
+}
+
+// Quantise one block by one wave: x[j][half] are its numbers.
+template <bool F8, int HD>
+__device__ __forceinline__ void quantise(const u32x4 (&x)[HD / 32][2], uint8_t *codes, float *scale, int lane)
 {
     constexpr int NJ = HD / 32;
-    u32x4 x[NJ][2];
     uint32_t m = 0;
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) {
-        x[j][0] = get(j, 0);
-        x[j][1] = get(j, 1);
-    }
 #pragma unroll
     for (int j = 0; j < NJ; ++j) m = max_bits(max_bits(m, x[j][0]), x[j][1]);
     const BlockScale b = block_scale<F8>(wave_max(m));
@@ -144,23 +148,57 @@ __device__ __forceinline__ void quantise(Get get, uint8_t *codes, float *scale, 
     if (lane == 0) *scale = b.scale;
 }
 
-// Slots [s0, s1) of eight slots of a dim of V, the first of them s; the others stay.
-__device__ __forceinline__ void copy_slots(uint16_t *to, const uint16_t *from, int s, int s0, int s1)
+// Eight slots of a dim of V: x's from slot `first` on, y's before
+__device__ __forceinline__ u32x4 join(const u32x4 &x, const u32x4 &y, int first)
 {
-    if (s >= s1 || s + 8 <= s0) return;
-    u32x4 x = *reinterpret_cast<const u32x4 *>(from);
-    if (s < s0 || s + 8 > s1) {
-        const u32x4 y = *reinterpret_cast<const u32x4 *>(to);
+    u32x4 r;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint32_t take = 0;
-            if (s + 2 * i >= s0 && s + 2 * i < s1) take |= 0xffffu;
-            if (s + 2 * i + 1 >= s0 && s + 2 * i + 1 < s1) take |= 0xffff0000u;
-            x[i] = (x[i] & take) | (y[i] & ~take);
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t old = (2 * i < first ? 0xffffu : 0u) | (2 * i + 1 < first ? 0xffff0000u : 0u);
+        r[i] = (y[i] & old) | (x[i] & ~old);
+    }
+    return r;
+}
+
+// Slots [s0, s1) of 32 slots of one head by one wave, K rows or a V tile; the others stay.
+// All is read before anything is written, so that one latency is paid, not eight.
+template <int HD> struct CopySlots {
+    static constexpr int N = HD / 16;
+    u32x4 x[N];
+    // K: rows, slot by slot.  V: octets of slots, those at the ends joined with what is there
+    __device__ __forceinline__ void read(const uint16_t *to, const uint16_t *from, bool is_v, int s0, int s1, int lane)
+    {
+        if (is_v) {
+            u32x4 y[N];
+            const int s = 8 * (lane & 3);
+            const bool some = s < s1 && s + 8 > s0, whole = s >= s0 && s + 8 <= s1;
+            if (some) {
+#pragma unroll
+                for (int k = 0; k < N; ++k) x[k] = *reinterpret_cast<const u32x4 *>(from + (lane + 64 * k) * 8);
+            }
+            if (some && !whole) {
+#pragma unroll
+                for (int k = 0; k < N; ++k) y[k] = *reinterpret_cast<const u32x4 *>(to + (lane + 64 * k) * 8);
+#pragma unroll
+                for (int k = 0; k < N; ++k) x[k] = join(y[k], join(x[k], y[k], s0 - s), s1 - s);
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < N; ++k) {
+                const int e = lane + 64 * k, s = e / (HD / 8);
+                if (s >= s0 && s < s1) x[k] = *reinterpret_cast<const u32x4 *>(from + e * 8);
+            }
         }
     }
-    *reinterpret_cast<u32x4 *>(to) = x;
-}
+    __device__ __forceinline__ void write(uint16_t *to, bool is_v, int s0, int s1, int lane) const
+    {
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int e = lane + 64 * k, s = is_v ? 8 * (lane & 3) : e / (HD / 8);
+            if (s < s1 && s + (is_v ? 8 : 1) > s0) *reinterpret_cast<u32x4 *>(to + e * 8) = x[k];
+        }
+    }
+};
 
 // ---------------------------------------------------------------------------
 // Store: a wave per block and per K or V (blockIdx.y), four to a workgroup.  The
@@ -169,11 +207,13 @@ __device__ __forceinline__ void copy_slots(uint16_t *to, const uint16_t *from, i
 //
 // A block is a wave's registers: 16 bytes per lane and load, one maximum over the
 // wave, 16 bytes of codes per lane and store, in the operands' order.  So nothing goes
-// through LDS and the rows are read once.  Bound by memory: 2 bytes read and 1 written
-// per number, none of them used again here, so they go past the caches (1024 rows of a
-// 13B model's 1600 heads, 1.26 GB: 206 us, 6.1 TB/s; through them 220).  150 rows of 1024
-// heads (129 MB) take 32.5 us (37.5), 4.0 TB/s: a wave has one block, which is loaded,
-// reduced and stored with nothing else in flight; few rows take a launch, 3.7 us.
+// through LDS and the rows are read once, K by whole lines (by half ones 3% longer).
+// Bound by memory: 2 bytes read and 1 written per number, none of them used again here, so
+// they go past the caches (through them 6% longer).  1024 rows of a 13B model's 1600 heads
+// (1.26 GB) 195 us, 6.5 TB/s, where the same bytes moved by nothing but loads and stores
+// take 191; 160 rows of 1024 heads (126 MB) 24 us, 5.2 TB/s (21).  Rows that begin and end
+// inside a block cost the old tail, which is read, and V's tiles, whose lines hold all 32
+// slots: 150 rows behind 333 30 us.  Few rows take a launch, 3.5 us.
 
 struct StoreArgs {
     KvqLayers c;
@@ -184,67 +224,62 @@ struct StoreArgs {
 
 template <bool F8, int HD> __global__ __launch_bounds__(256) void k_kvq_store(StoreArgs a)
 {
-    const int lane = threadIdx.x & 63;
-    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    constexpr int NJ = HD / 32;
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (w >= (int64_t)a.c.L * a.c.H * a.jobs) return;
     const int64_t lh = w / a.jobs;
     const int job = (int)(w - lh * a.jobs);
     const bool is_v = blockIdx.y != 0;
-    const int b0 = a.c.len / KVQ_BLOCK, r = a.c.len % KVQ_BLOCK, n = lane & 15, g = lane >> 4;
+    const int b0 = a.c.len / KVQ_BLOCK, r = a.c.len % KVQ_BLOCK;
     uint16_t *tail = (is_v ? a.c.v_tail : a.c.k_tail) + lh * KVQ_TAIL * HD;
     const uint16_t *rows = (is_v ? a.from.v : a.from.k) + lh * a.from.cap * HD;
+    u32x4 x[NJ][2];
     if (job < a.full) {
-        const int64_t at = lh * a.c.nb + b0 + job;
-        uint8_t *codes = (is_v ? a.c.v : a.c.k) + at * KVQ_BLOCK * HD;
-        float *scale = a.c.scale + at * 2 + is_v;
         const int old = job == 0 ? r : 0;  // rows that the tail holds
-        if (is_v) {
-            const uint16_t *tile = rows + (size_t)(b0 + job) * KVQ_BLOCK * HD;
-            quantise<F8, HD>(
-                [&](int j, int half) {
-                    const int e = (32 * j + 16 * half + n) * 32 + 8 * g;
-                    u32x4 x = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(tile + e));
-                    if (8 * g < old) {
-                        const u32x4 y = *reinterpret_cast<const u32x4 *>(tail + e);
+        const uint16_t *block = rows + (size_t)(b0 + job) * KVQ_BLOCK * HD;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const uint32_t keep = (8 * g + 2 * i < old ? 0xffffu : 0u) | (8 * g + 2 * i + 1 < old ? 0xffff0000u : 0u);
-                            x[i] = (y[i] & keep) | (x[i] & ~keep);
-                        }
-                    }
-                    return x;
-                },
-                codes, scale, lane);
-        } else {
-            quantise<F8, HD>(
-                [&](int j, int half) {
-                    const int s = k_slot(lane, j & 1), d = 64 * (j >> 1) + 32 * half + 8 * g;
-                    const uint16_t *p = s < old ? tail + s * HD : rows + (size_t)((b0 + job) * KVQ_BLOCK + s) * HD;
-                    return __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(p + d));
-                },
-                codes, scale, lane);
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const int s = is_v ? 8 * g : k_slot(lane & 55 | 8 * half, j & 1);
+                const int e = is_v ? (32 * j + 16 * half + n) * 32 + s : s * HD + 64 * (j >> 1) + 4 * (n & 8) + 8 * g;
+                x[j][half] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>((s < old ? tail : block) + e));
+            }
+        if (!is_v)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) swap_halves(x[j][0], x[j][1], n & 8);
+        if (is_v && old > 8 * g && old < 8 * g + 8) {  // old and new slots in one octet
+            u32x4 y[NJ][2];
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+                    y[j][half] = *reinterpret_cast<const u32x4 *>(block + (32 * j + 16 * half + n) * 32 + 8 * g);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+#pragma unroll
+                for (int half = 0; half < 2; ++half) x[j][half] = join(y[j][half], x[j][half], old - 8 * g);
         }
     }
-    if (job != 0) return;
     // tail slots [s0, s1): the rows behind the last whole block
-    const int b1 = b0 + a.full, s0 = a.full ? 0 : r, s1 = a.c.len + a.n - b1 * KVQ_BLOCK;
-    if (s1 <= s0) return;
-    if (is_v) {
-        const uint16_t *tile = rows + (size_t)b1 * KVQ_BLOCK * HD;
-#pragma unroll
-        for (int e = lane; e < HD * 4; e += 64) copy_slots(tail + e * 8, tile + e * 8, 8 * (e & 3), s0, s1);
-    } else {
-        const uint16_t *first = rows + (size_t)b1 * KVQ_BLOCK * HD;
-        for (int e = s0 * HD / 8 + lane; e < s1 * HD / 8; e += 64)
-            *reinterpret_cast<u32x4 *>(tail + e * 8) = *reinterpret_cast<const u32x4 *>(first + e * 8);
+    const int b1 = b0 + a.full, s0 = a.full ? 0 : r, s1 = job == 0 ? a.c.len + a.n - b1 * KVQ_BLOCK : 0;
+    CopySlots<HD> rest;
+    if (s1 > s0) rest.read(tail, rows + (size_t)b1 * KVQ_BLOCK * HD, is_v, s0, s1, lane);
+    if (job < a.full) {
+        const int64_t at = lh * a.c.nb + b0 + job;
+        quantise<F8, HD>(x, (is_v ? a.c.v : a.c.k) + at * KVQ_BLOCK * HD, a.c.scale + at * 2 + is_v, lane);
     }
+    if (s1 > s0) rest.write(tail, is_v, s0, s1, lane);
 }
 
 // ---------------------------------------------------------------------------
 // Load: a wave per block, the tail's committed rows as one more; store backwards, 1 byte
 // read and 2 written per number.  Bound by memory: 8191 slots of 320 heads (2.0 GB)
-// 393 us, 5.1 TB/s; 333 slots of 1024 heads (265 MB) 54.5 us, 4.9 TB/s, and through the
-// caches 61.
+// 336 us, 6.0 TB/s; 333 slots of 1024 heads (265 MB) 46.5 us, 5.7 TB/s.  K is written by
+// whole lines (by half ones 12% longer), all of it past the caches (through them 10%
+// longer); the conversion is 2.5 instructions a number (with a rounding to bf16 by
+// integers four times that, and 4% longer).
 //
 // A number is its code x scale, rounded to fp32 and then to bf16, the cache's type: two
 // roundings of 2^-24 and 2^-8, beside a code's own of up to half a step.
@@ -259,7 +294,7 @@ template <bool F8, int HD> __global__ __launch_bounds__(256) void k_kvq_load(Loa
 {
     constexpr int NJ = HD / 32;
     const int lane = threadIdx.x & 63;
-    const int64_t w = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (w >= (int64_t)a.c.L * a.c.H * a.jobs) return;
     const int64_t lh = w / a.jobs;
     const int b = (int)(w - lh * a.jobs), blocks = a.c.len / KVQ_BLOCK, r = a.c.len % KVQ_BLOCK;
@@ -275,25 +310,26 @@ template <bool F8, int HD> __global__ __launch_bounds__(256) void k_kvq_load(Loa
 #pragma unroll
         for (int j = 0; j < NJ; ++j) x[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(codes + (j * 64 + lane) * 16));
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
+        for (int j = 0; j < NJ; ++j) {
+            u32x4 y[2];
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-                const u32x4 y = scaled_bf16(bf16_of<F8>(x[j][2 * half], x[j][2 * half + 1]), scale);
-                const int e = is_v ? (32 * j + 16 * half + n) * 32 + 8 * g
-                                   : k_slot(lane, j & 1) * HD + 64 * (j >> 1) + 32 * half + 8 * g;
-                __builtin_nontemporal_store(y, reinterpret_cast<u32x4 *>(to + e));
+            for (int half = 0; half < 2; ++half) y[half] = scaled_bf16<F8>(x[j][2 * half], x[j][2 * half + 1], scale);
+            if (is_v) {
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+                    __builtin_nontemporal_store(y[half], reinterpret_cast<u32x4 *>(to + (32 * j + 16 * half + n) * 32 + 8 * g));
+            } else {
+                swap_halves(y[0], y[1], n & 8);
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+                    __builtin_nontemporal_store(y[half], reinterpret_cast<u32x4 *>(to + k_line(lane, j, half, HD)));
             }
+        }
         return;
     }
-    if (is_v) {
-        const uint16_t *tail = a.c.v_tail + lh * KVQ_TAIL * HD;
-#pragma unroll
-        for (int e = lane; e < HD * 4; e += 64) copy_slots(to + e * 8, tail + e * 8, 8 * (e & 3), 0, r);
-    } else {
-        const uint16_t *tail = a.c.k_tail + lh * KVQ_TAIL * HD;
-        for (int e = lane; e < r * HD / 8; e += 64)
-            *reinterpret_cast<u32x4 *>(to + e * 8) = *reinterpret_cast<const u32x4 *>(tail + e * 8);
-    }
+    CopySlots<HD> x;
+    x.read(to, (is_v ? a.c.v_tail : a.c.k_tail) + lh * KVQ_TAIL * HD, is_v, 0, r, lane);
+    x.write(to, is_v, 0, r, lane);
 }
 
 // ---------------------------------------------------------------------------
