@@ -108,7 +108,6 @@ KvqAttnArgs attention_args(const dv_kvq *c, int layer, int n)
 // The cut, and its parts of the workspace.
 void set_cut(KvqAttnArgs &a, const KvqCut &cut, int hd, void *ws)
 {
-    a.per_split = cut.per_split;
     a.o.n_split = cut.n_split;
     a.o.part_o = static_cast<float *>(ws);
     a.o.part_ml = reinterpret_cast<float2 *>(a.o.part_o + (size_t)a.o.H * cut.n_split * a.o.rows * hd);

@@ -37,22 +37,25 @@ hipError_t launch_kvq_load(const KvqLayers &c, const KvqRows &to, hipStream_t s)
 hipError_t launch_kvq_advance(const KvqLayers &c, const int32_t *path, int n, hipStream_t s);
 
 // How a call's keys are cut: row tiles of up to 16 rt query rows (a KV head's n x
-// group rows) in z groups, n_split ranges of per_split 32-key tiles each.  A workgroup's
-// 8 waves take a tile each at a time, so z n_split heads is about the CUs.
+// group rows) in z groups, n_split shares of the 32-key tiles.  A workgroup's 8 waves take
+// a tile each at a time, so z n_split heads is about the CUs.  Shares are dealt in groups
+// of 8 tiles in turn, so that the workgroups of a head read side by side: where each has
+// a range of its own, their distances can fall on the same memory channels (8 heads x 32
+// rows, 130001 slots: 61 to 66 us as ranges, by where the cache lies, 55 to 56 dealt).
 //
 // rt 2 reads and converts a tile once for 32 rows, rt 1 has twice the workgroups and no
 // waiting for the longer sums: 1 up to 12 tiles a wave.  us by tiles a wave, rt 1 / 2: 2.0
 // (8 heads x 32 rows, 8192 slots) 11.5 / 15.5, 5.2 (40 x 60, 2077) 15.1 / 18.1, 8.0 (8 x 64,
 // 16384) 18.6 / 20.5, 16 (32 x 32, 16384) 32.1 / 30.1, 32 (8 x 32, 130001) 58 / 55.
 //
-// Ranges of less than 8 tiles leave waves idle, and several ranges cost a second launch,
-// so up to 24 tiles stay one: 17 tiles of 32 heads 7.6 us as one range, 8.7 as three; 22 of 8
+// Shares of less than 8 tiles leave waves idle, and several shares cost a second launch,
+// so up to 24 tiles stay one: 17 tiles of 32 heads 7.6 us as one share, 8.7 as three; 22 of 8
 // heads 8.8 and 8.7; 34 of 40 heads 10.3 and 10.0; 32 of 8 heads 9.9 and 8.6.
 struct KvqCut {
-    int rt, z, per_split, n_split;
+    int rt, z, n_split;
 };
 inline int kvq_row_groups(int rows, int rt) { return (rows + 16 * rt - 1) / (16 * rt); }
-// the most ranges of any cache length
+// the most shares of any cache length
 inline int kvq_max_split(int heads, int rows, int n_cu)
 {
     const int most = n_cu / (heads * kvq_row_groups(rows, 2));
@@ -63,19 +66,18 @@ inline KvqCut kvq_cut(int heads, int rows, int tiles, int n_cu)
     KvqCut c;
     c.rt = (double)tiles * heads * kvq_row_groups(rows, 1) > 12. * 8 * n_cu && rows > 16 ? 2 : 1;
     c.z = kvq_row_groups(rows, c.rt);
-    const int most = tiles <= 24 ? 1 : n_cu / (heads * c.z) > 1 ? n_cu / (heads * c.z) : 1;
-    c.per_split = (tiles + most - 1) / most > 8 ? (tiles + most - 1) / most : 8;
-    c.n_split = (tiles + c.per_split - 1) / c.per_split;
+    const int most = tiles <= 24 ? 1 : n_cu / (heads * c.z) > 1 ? n_cu / (heads * c.z) : 1, groups = (tiles + 7) / 8;
+    c.n_split = most < groups ? most : groups;
     return c;
 }
-// Workspace of n_split ranges (one writes the output itself): partial sums, and a
+// Workspace of n_split shares (one writes the output itself): partial sums, and a
 // reference and sum of weights for each.
 inline size_t kvq_attention_bytes(int heads, int rows, int hd, int n_split)
 {
     return n_split == 1 ? 0 : (size_t)heads * n_split * rows * (hd + 2) * 4;
 }
 
-// Where attention's sums go: the output, or ranges to be combined.
+// Where attention's sums go: the output, or shares to be combined.
 struct KvqOut {
     float *out;                  // [n][H G][hd], row stride ldo, or
     int64_t ldo;
@@ -96,7 +98,7 @@ struct KvqAttnArgs {
     int32_t r, n;                // committed and new rows of the tail
     const float *q;              // [n][H G][hd], row stride ldq
     int64_t ldq;
-    int32_t tiles, per_split;
+    int32_t tiles;
     KvqOut o;
     uint64_t mask[KVQ_MAX_NEW];  // bit j: new row i sees new row j
 };

@@ -474,11 +474,11 @@ template <bool F8, int HD> __global__ __launch_bounds__(256, 6) void k_kvq_advan
 //   ones, and new row j where bit j of its mask is set;
 //   o_i = sum_j exp(s_ij - m_i) v_j / sum_j exp(s_ij - m_i), 0 if it sees none.
 //
-// Workgroup (split, KV head, row group): its waves take interleaved 32-key tiles of
-// the range (blocks of codes, then up to three tiles of the tail) with a running
-// reference m and sum per query row, and are combined in LDS; a second launch combines
-// the ranges, in their order.  Rows are the n new tokens x the G query heads that share
-// the KV head.
+// Workgroup (split, KV head, row group): its share of the 32-key tiles (blocks of codes,
+// then up to three tiles of the tail) is groups of eight in turn, a tile a wave, each with
+// a running reference m and sum per query row.  The waves are combined in LDS; a second
+// launch combines the shares, in their order.  Rows are the n new tokens x the G query
+// heads that share the KV head.
 //
 //   S^T = K Q^T: A = 16 keys x dims, B = queries; D gives lane (n, g) the scores of
 //   row n for the 8 consecutive keys 8 g .. +8 of the tile, which are the B operand
@@ -511,8 +511,8 @@ template <bool F8, int HD> __global__ __launch_bounds__(256, 6) void k_kvq_advan
 // K (V is converted by then): 64 KB per CU in flight while weights and sums are made.
 // Times, with the merge where there is one, and with two tiles in flight in two sets of
 // registers, which is twice the code and no faster but for a single tile a wave:
-//   8 heads x 32 rows, 130001 slots (267 MB)  55.5 us (58.4), 4.8 TB/s; reading alone,
-//                                             this way cut, 45, and the merge 4
+//   8 heads x 32 rows, 130001 slots (267 MB)  55.5 us (58), 4.8 TB/s; reading alone, this
+//                                             way cut, 41 to 45, and the merge 4.5
 //   32 heads x 1 row, 8191 slots (67 MB)      17.6 (18.1): reading alone 12.4, merge
 //   40 heads x 60 rows, 2077 slots, e4m3      15.0 (16.0): 160 workgroups, 9 tiles a wave
 //   40 heads x 16 rows, 1037 slots (12 MB)    10.0 (9.9): latencies of 1 tile a wave, merge
@@ -653,8 +653,10 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
 #pragma unroll
         for (int j = 0; j < NC; ++j) x.v[j] = __builtin_nontemporal_load(reinterpret_cast<const u32x4 *>(vp + j * 1024));
     };
-    const int t0 = split * a.per_split, t1 = min(a.tiles, t0 + a.per_split), c1 = min(t1, a.blocks);
-    const bool has_tail = t1 > a.blocks;
+    // the wave's tiles: every step-th from t0 on, codes below a.blocks and then at most one of
+    // the tail's (there are three, in two groups)
+    const int t0 = split * NW + wave, step = a.o.n_split * NW;
+    const bool has_tail = a.blocks / NW % a.o.n_split == split || (a.tiles - 1) / NW % a.o.n_split == split;
     Raw buf0, buf1;  // (buf1: a tail tile's other half, which is twice a tile of codes)
 
     // 8 dims of one row per thread; a row's threads are neighbours.  (Loads return in
@@ -689,13 +691,13 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
         fetch(k1, 64, v0 + NC * 1024, buf1);
     };
     // The wave's first tile, codes or tail, without a branch: the queries' wait then leaves
-    // these loads in flight.  (A wave without a tile takes the range's first, which is
-    // somewhere in the buffers, and does not use it.)
-    const bool tail_first = t0 + wave >= c1;
+    // these loads in flight.  (A wave without a tile takes one that is there and
+    // does not use it.)
+    const bool tail_first = t0 >= a.blocks;
     {
         const char *k0, *k1, *v0;
-        tail_at(max(min(t0 + wave, t1 - 1), a.blocks), k0, k1, v0);
-        const int64_t at = (int64_t)h * a.nb + (tail_first ? 0 : t0 + wave);
+        tail_at(max(min(t0, a.tiles - 1), a.blocks), k0, k1, v0);
+        const int64_t at = (int64_t)h * a.nb + (tail_first ? 0 : t0);
         const char *kc = reinterpret_cast<const char *>(a.k + at * KVQ_BLOCK * HD + lane * 16);
         const char *vc = reinterpret_cast<const char *>(a.v + at * KVQ_BLOCK * HD + lane * 16);
         buf0.s = a.scale[at * 2 + (lane & 1)];
@@ -745,9 +747,9 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
             for (int p = 0; p < 3; ++p) qt[row / 16][(c * 3 + p) * 64 + at] = t[p];
         }
     }
-    if (tail_first && t0 + wave < t1) {
+    if (tail_first && t0 < a.tiles) {
         const char *k0, *k1, *v0;
-        tail_at(t0 + wave, k0, k1, v0);
+        tail_at(t0, k0, k1, v0);
         fetch(k1, 64, v0 + NC * 1024, buf1);
     }
     uint64_t mask[RT];
@@ -821,7 +823,7 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
         each<RT>([&](auto rt_) {
             constexpr int rt = decltype(rt_)::value;
             if (RT > 1 && row0 + 16 * rt >= rows) {
-                if (rt == RT - 1 && next < c1) load(next, x);
+                if (rt == RT - 1 && next < a.blocks) load(next, x);
                 return;
             }
             float s[8];
@@ -852,7 +854,7 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
                     s[4 + i] = fmaf((float)sb[2][i], 65536.f, (float)(sb[1][i] * 256 + sb[0][i]));
                 }
             }
-            if (rt == RT - 1 && next < c1) load(next, x);
+            if (rt == RT - 1 && next < a.blocks) load(next, x);
             const float c = coef[rt] * k_scale;
             float mt = s[0];
 #pragma unroll
@@ -876,14 +878,13 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
             }
         });
     };
-    for (int t = t0 + __builtin_amdgcn_readfirstlane(wave); t < c1; t += NW) codes(buf0, t + NW);
+    int t = __builtin_amdgcn_readfirstlane(t0);
+    for (; t < a.blocks; t += step) codes(buf0, t + step);
 
-    // tail tiles of the range, by the waves whose turn it is
-    const int tt = max(t0, a.blocks);
-    for (int t = tt + (wave + NW - (tt - t0) % NW) % NW; t < t1; t += NW) {
+    if (t < a.tiles) {  // a tile of the tail
         const int s0 = (t - a.blocks) * KVQ_BLOCK, left = min(KVQ_BLOCK, a.r + a.n - s0);
         const uint16_t *vt = a.vt + ((int64_t)h * KVQ_TAIL + s0) * HD;
-        if (t != t0 + wave) load_tail(t);
+        if (!tail_first) load_tail(t);
         u32x4 v[ND];
         // V without the slots past the last row, which hold anything
         const int mine = min(max(left - 8 * g, 0), 8);  // of the lane's 8 keys
@@ -1019,8 +1020,8 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
     }
 }
 
-// The ranges combined, in a launch of its own: 4 threads share a row's 4 dims, each with
-// every fourth range, and are combined in LDS.  The order is fixed, so are the results.
+// The shares combined, in a launch of its own: 4 threads share a row's 4 dims, each with
+// every fourth share, and are combined in LDS.  The order is fixed, so are the results.
 // 3.4 to 4.7 us, a launch and three dependent reads.  The last workgroup of a head
 // doing it in place of a launch was slower everywhere: it waits for its own writes and
 // for a counter, then merges alone (32 heads x 1 row, 8191 slots 18.7 us for 17.9; 8 x 32,
@@ -1042,7 +1043,7 @@ template <int HD> __global__ __launch_bounds__(256) void k_kvq_merge(KvqOut a)
             const float2 ml = a.part_ml[p];
             const f32x4 o4 = *reinterpret_cast<const f32x4 *>(a.part_o + p * HD + d0);
             const float ms = ml.x, ls = ml.y;
-            const float mx = fmaxf(m, ms);  // (a range that saw nothing, or only NaN, has no reference)
+            const float mx = fmaxf(m, ms);  // (a share that saw nothing, or only NaN, has no reference)
             const float f = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - mx);
             const float w = ms == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ms - mx);
             l = l * f + w * ls;

@@ -141,7 +141,7 @@ extern "C" void kvq_hush() { g_said.clear(); }
 extern "C" void kvq_cut_of(int heads, int rows, int tiles, int n_cu, int *out)
 {
     const KvqCut c = kvq_cut(heads, rows, tiles, n_cu);
-    out[0] = c.rt, out[1] = c.z, out[2] = c.per_split, out[3] = c.n_split, out[4] = kvq_max_split(heads, rows, n_cu);
+    out[0] = c.rt, out[1] = c.z, out[2] = c.n_split, out[3] = kvq_max_split(heads, rows, n_cu);
 }
 """
 
@@ -165,16 +165,15 @@ def lib(tmp_path_factory):
 
 
 @pytest.mark.parametrize("n_cu", [256, 64])
-def test_every_tile_is_in_one_range(lib, n_cu):
-    out = (ctypes.c_int * 5)()
+def test_every_row_and_every_share_has_work(lib, n_cu):
+    out = (ctypes.c_int * 4)()
     for heads in (1, 3, 8, 40, 300):
         for rows in (1, 16, 17, 33, 64, 65, 512):
-            for tiles in (1, 2, 3, 5, 32, 35, 257, 4100):
+            for tiles in (1, 2, 3, 5, 8, 24, 25, 32, 35, 257, 4100):
                 lib.kvq_cut_of(heads, rows, tiles, n_cu, out)
-                rt, z, per, n_split, most = out
+                rt, z, n_split, most = out
                 assert 16 * rt * z >= rows > 16 * rt * (z - 1)
-                assert per >= 1 and (n_split - 1) * per < tiles <= n_split * per
-                assert 1 <= n_split <= min(most, tiles)
+                assert 1 <= n_split <= min(most, (tiles + 7) // 8)    # dealt in groups of 8 tiles
 
 
 class KvqEngine(Engine):
