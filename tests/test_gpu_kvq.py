@@ -344,6 +344,26 @@ def test_attention(fmt, hd, len0, n, heads, group, kind):
         assert not got[::3].any()                     # rows that see nothing
 
 
+@pytest.mark.parametrize("fmt,hd", [("i8", 128), ("f8", 64)])
+@pytest.mark.parametrize("len0,n,heads", [(991, 64, 2), (1012, 60, 2), (1037, 2, 64), (1311, 50, 20)])
+def test_tail_tiles_of_different_shares(fmt, hd, len0, n, heads):
+    """Tail tiles 30..32 and 31..33, in groups of eight that go to different workgroups,
+    and tails that follow a workgroup's first tiles."""
+    rng = np.random.default_rng(len0)
+    p = Pair(1, heads, hd, 32 * (len0 // 32 + 4), fmt)
+    p.preset(rng, len0)
+    _check_attention(p, rng, n, 1, "tree")
+
+
+@pytest.mark.parametrize("fmt,hd,len0", [("i8", 64, 45), ("f8", 128, 300)])
+def test_the_most_query_heads_of_a_kv_head(fmt, hd, len0):
+    """65536 rows, 16 and 32 to a workgroup."""
+    rng = np.random.default_rng(len0)
+    p = Pair(1, 1, hd, 448, fmt)
+    p.preset(rng, len0)
+    _check_attention(p, rng, 64, 1024, "tree")
+
+
 @pytest.mark.parametrize("fmt,hd", [("i8", 64), ("f8", 64), ("i8", 128), ("f8", 128)])
 def test_attention_of_many_rows_over_a_long_cache(fmt, hd):
     """32 rows a workgroup (more than 12 tiles a wave), random codes."""
