@@ -50,7 +50,7 @@ def source_hash() -> str:
 
 
 def _short(name: str) -> str:
-    return name.replace("void ", "").split("(")[0]
+    return name.replace("void ", "").replace("(anonymous namespace)::", "").split("(")[0]
 
 
 def summarize_stats(stats_csv, trace_csv, out_path, command):
