@@ -504,6 +504,47 @@ def test_offsets_past_32_bits():
     assert torch.equal(*outs) and torch.isfinite(outs[0]).all()
 
 
+def test_moves_past_32_bits():
+    """Store, advance and read-back of the last layer where codes, rows and their products
+    lie beyond 4 GiB: as a cache of that layer alone."""
+    nl, nh, hd, cap = 9, 64, 128, 65536
+    need = 6 * nl * nh * cap * hd
+    if torch.cuda.mem_get_info()[0] < 2 * need:
+        pytest.skip("needs %d GiB" % (2 * need >> 30))
+    g = torch.Generator(device=DEV).manual_seed(2)
+    done = []
+    for layers in (1, nl):
+        c = D.DeviceKVQ(1, 1, 64, 32, "f8")
+        for name, shape, dt in (("k", (cap // 32, 32 * hd), torch.int8), ("v", (cap // 32, 32 * hd), torch.int8),
+                                ("scale", (cap // 32, 2), torch.float32), ("k_tail", (96, hd), torch.bfloat16),
+                                ("v_tail", (3, hd, 32), torch.bfloat16)):
+            t = torch.empty((layers, nh) + shape, dtype=dt, device=DEV)
+            if dt == torch.int8:
+                t[-1].fill_(0x31)
+            else:
+                t[-1].normal_(generator=g.manual_seed(len(name)))
+            setattr(c, name, t)
+        c.c = dv.dv_kvq(c.k.data_ptr(), c.v.data_ptr(), c.scale.data_ptr(), c.k_tail.data_ptr(), c.v_tail.data_ptr(),
+                        layers, nh, hd, dv.DV_F8, cap, cap - 150)
+        k = torch.empty((layers, nh, cap, hd), dtype=torch.bfloat16, device=DEV)
+        v = torch.empty((layers, nh, cap // 32, hd, 32), dtype=torch.bfloat16, device=DEV)
+        for t, seed in ((k, 5), (v, 6)):
+            t[-1].normal_(generator=g.manual_seed(seed))
+        kv = dv.dv_kv(k.data_ptr(), v.data_ptr(), cap, cap)
+        dv.dv_kvq_store(c.c, kv, 101)
+        dv.dv_kvq_advance(c.c, list(range(3, 23)) + [40])
+        codes = [getattr(c, name)[-1].clone() for name in ("k", "v", "scale", "k_tail", "v_tail")]
+        dv.dv_kvq_load(c.c, kv)
+        torch.cuda.synchronize()
+        assert c.len == kv.len == cap - 28
+        done.append(codes + [k[-1].clone(), v[-1].clone()])
+        del c, k, v, t
+        torch.cuda.empty_cache()
+    assert (nl - 1) * nh * cap * hd >= 1 << 32       # (the last layer's first code)
+    for a, b in zip(*done):
+        assert torch.equal(a.view(torch.int8), b.view(torch.int8))
+
+
 def test_streams_and_graphs():
     """On a stream of the caller's, and captured: every replay as the eager call, with
     other inputs in the same buffers and eager work in between."""
