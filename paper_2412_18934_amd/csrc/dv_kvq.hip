@@ -491,18 +491,21 @@ template <bool F8, int HD> __global__ __launch_bounds__(256, 6) void k_kvq_advan
 //     the products are exact integers, and K's bytes are operands as they stand;
 //   e4m3 K: q in two fp16 (11 + 11 bits), its row scaled to a largest of 2^10 .. 2^11
 //     so that the low part stays normal; e4m3 is exact in fp16;
-//   V: weights in two fp16; int8 and e4m3 are exact in fp16;
-//   tail: bf16, whose range fp16 has not; q and weights in three bf16 (8 + 8 + 8).
+//   V: weights in three bf16 (8 + 8 + 8 bits: all of them); int8 and e4m3 are exact in bf16;
+//   tail: q and weights in three bf16.
 // Weights are exp2(s - m) with m a reference that a row's scores exceed by at most
 // LAZY (in base 2): it moves, and the sums are rescaled, only when a score is further
 // above it, which after the first tiles is rare.  V's scales likewise: the sums are
-// in units of the largest scale so far.  So a weight is at most 2^(LAZY + 11) = 2^15 in
-// fp16, which holds 65504.
+// in units of the largest scale so far, and 2^-32 of that (W_UNIT), so that a weight times its
+// scale is a normal number while scales differ by up to 2^126, and the sums stay far
+// below fp32's end.
 //
-// Roundings: a query to 2^-23 of its row's largest (int8) or 2^-22 of itself (e4m3), a
-// weight to 2^-22 of itself or 2^-35 of the largest a row can have; products and sums are
-// fp32 (int8 scores integers).  Against 64 bits the outputs are about as near as a
-// plain fp32 computation's.
+// Roundings: a query to 2^-23 of its row's largest (int8) or 2^-22 of itself (e4m3);
+// weights, products and sums are fp32 (int8 scores integers).  Against 64 bits the outputs
+// are about as near as a plain fp32 computation's.  (Weights in two fp16, which have 22 bits
+// and an end at 2^-24 of the unit, lost those of small weights and of blocks whose
+// scale is small beside an earlier one's: 23% of an output at a ratio of 2^36.  Three bf16
+// cost nothing with few rows, 8 to 11% with many.)
 //
 // What bounds it: with few rows the codes' bytes (2 hd + 8 / 32 per key and head); with
 // more, the conversion of V and the parts' matrix instructions, which come per tile and
@@ -521,7 +524,7 @@ template <bool F8, int HD> __global__ __launch_bounds__(256, 6) void k_kvq_advan
 // at the matrix instructions, more independent chains of them, V asked for before the
 // scores: each equal or slower.
 
-constexpr float LAZY = 4.f, W_UNIT = 2048.f;
+constexpr float LAZY = 4.f, W_UNIT = 0x1p32f;
 
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -529,22 +532,28 @@ typedef int i32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ uint32_t bits_of(f16x2 x) { return __builtin_bit_cast(uint32_t, x); }
 
-// Eight codes as fp16.  int8: 0x6400 + (code + 128) is 1024 + 128 + code.
-template <bool F8> __device__ __forceinline__ u32x4 f16_of(uint32_t lo, uint32_t hi)
+// Eight e4m3 codes as fp16
+__device__ __forceinline__ u32x4 f16_of(uint32_t lo, uint32_t hi)
+{
+    return (u32x4){bits_of((f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false)),
+                   bits_of((f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true)),
+                   bits_of((f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false)),
+                   bits_of((f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true))};
+}
+
+// Eight codes as bf16: at most 8 bits each, so exact
+template <bool F8> __device__ __forceinline__ u32x4 bf16_of(uint32_t lo, uint32_t hi)
 {
     u32x4 r;
-    if constexpr (F8) {
-        r[0] = bits_of((f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, false));
-        r[1] = bits_of((f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.f, true));
-        r[2] = bits_of((f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, false));
-        r[3] = bits_of((f16x2)__builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.f, true));
-    } else {
-        const f16x2 off = {(_Float16)-1152.f, (_Float16)-1152.f};
-        const uint32_t w[2] = {lo ^ 0x80808080u, hi ^ 0x80808080u};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t x = __builtin_amdgcn_perm(0x64646464u, w[i >> 1], i & 1 ? 0x07030702u : 0x07010700u);
-            r[i] = bits_of(__builtin_bit_cast(f16x2, x) + off);
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w = i < 2 ? lo : hi;
+        if constexpr (F8) {
+            r[i] = __builtin_bit_cast(uint32_t, i & 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, true)
+                                                      : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.f, false));
+        } else {
+            const f32x2 x = {(float)(int8_t)(w >> (16 * (i & 1))), (float)(int8_t)(w >> (16 * (i & 1) + 8))};
+            r[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
         }
     }
     return r;
@@ -762,7 +771,7 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
 
     float m_run[RT], l_run[RT], coef[RT];  // (l_run: of the lane's own keys)
     f32x4 o[RT][ND];
-    float v_unit = 0.f, v_inv = 0.f;
+    float v_unit = 0x1p-64f, v_inv = 0x1p64f;
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         m_run[rt] = -INFINITY;
@@ -810,15 +819,15 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
 #pragma unroll
         for (int j = 0; j < NC; ++j)
 #pragma unroll
-            for (int half = 0; half < 2; ++half) v[2 * j + half] = f16_of<F8>(x.v[j][2 * half], x.v[j][2 * half + 1]);
+            for (int half = 0; half < 2; ++half) v[2 * j + half] = bf16_of<F8>(x.v[j][2 * half], x.v[j][2 * half + 1]);
         u32x4 ka[NC], kb[NC];  // e4m3 as fp16
         if constexpr (F8)
 #pragma unroll
             for (int j = 0; j < NC / 2; ++j)
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    ka[2 * j + half] = f16_of<true>(x.k[2 * j][2 * half], x.k[2 * j][2 * half + 1]);
-                    kb[2 * j + half] = f16_of<true>(x.k[2 * j + 1][2 * half], x.k[2 * j + 1][2 * half + 1]);
+                    ka[2 * j + half] = f16_of(x.k[2 * j][2 * half], x.k[2 * j][2 * half + 1]);
+                    kb[2 * j + half] = f16_of(x.k[2 * j + 1][2 * half], x.k[2 * j + 1][2 * half + 1]);
                 }
         each<RT>([&](auto rt_) {
             constexpr int rt = decltype(rt_)::value;
@@ -869,13 +878,12 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
                 w[i] *= vs;
             }
             l_run[rt] += ps;
-            u32x4 p2[2];
-            split2(w, p2);
+            u32x4 p3[3];
+            split3(w, p3);
 #pragma unroll
-            for (int dt = 0; dt < ND; ++dt) {
-                o[rt][dt] = mfma_f16(v[dt], p2[0], o[rt][dt]);
-                o[rt][dt] = mfma_f16(v[dt], p2[1], o[rt][dt]);
-            }
+            for (int p = 0; p < 3; ++p)
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt) o[rt][dt] = mfma_bf16(v[dt], p3[p], o[rt][dt]);
         });
     };
     int t = __builtin_amdgcn_readfirstlane(t0);
