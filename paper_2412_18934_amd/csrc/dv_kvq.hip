@@ -489,8 +489,8 @@ template <bool F8, int HD> __global__ __launch_bounds__(256, 6) void k_kvq_advan
 // Each query and weight is one fp32 number in parts:
 //   int8 K: q as a 23-bit integer relative to its row's largest, in three signed bytes;
 //     the products are exact integers, and K's bytes are operands as they stand;
-//   e4m3 K: q in two fp16 (11 + 11 bits), its row scaled to a largest of 2^10 .. 2^11
-//     so that the low part stays normal; e4m3 is exact in fp16;
+//   e4m3 K: q in two fp16 (11 + 11 bits and a sign between), its row scaled to a largest of
+//     2^10 .. 2^11 so that the low part stays normal; e4m3 is exact in fp16;
 //   V: weights in three bf16 (8 + 8 + 8 bits: all of them); int8 and e4m3 are exact in bf16;
 //   tail: q and weights in three bf16.
 // Weights are exp2(s - m) with m a reference that a row's scores exceed by at most
@@ -500,7 +500,8 @@ template <bool F8, int HD> __global__ __launch_bounds__(256, 6) void k_kvq_advan
 // scale is a normal number while scales differ by up to 2^126, and the sums stay far
 // below fp32's end.
 //
-// Roundings: a query to 2^-23 of its row's largest (int8) or 2^-22 of itself (e4m3);
+// Roundings: a query to 2^-22 of its row's largest (int8: half a step of an integer of at
+// least 2^21) or 2^-23 of itself and 2^-35 of its row's largest (e4m3);
 // weights, products and sums are fp32 (int8 scores integers).  Against 64 bits the outputs
 // are about as near as a plain fp32 computation's.  (Weights in two fp16, which have 22 bits
 // and an end at 2^-24 of the unit, lost those of small weights and of blocks whose
@@ -580,16 +581,15 @@ __device__ __forceinline__ void split3(const float *v, u32x4 (&t)[3])
     }
 }
 
-// Eight fp32 numbers of at most 65504 as two fp16 each, by truncation: 2^-22 of the
-// number, or 2^-24, is lost at most.
+// Eight fp32 numbers of at most 2^15 as two fp16 each, to the nearest: off by at most 2^-23
+// of the number, or 2^-25 (half of fp16's smallest).
 __device__ __forceinline__ void split2(const float *v, u32x4 (&t)[2])
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const f16x2 h = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_pkrtz(v[2 * i], v[2 * i + 1]));
+        const f16x2 h = {(_Float16)v[2 * i], (_Float16)v[2 * i + 1]};
         t[0][i] = bits_of(h);
-        t[1][i] = bits_of(__builtin_bit_cast(
-            f16x2, __builtin_amdgcn_cvt_pkrtz(v[2 * i] - (float)h[0], v[2 * i + 1] - (float)h[1])));
+        t[1][i] = bits_of((f16x2){(_Float16)(v[2 * i] - (float)h[0]), (_Float16)(v[2 * i + 1] - (float)h[1])});
     }
 }
 
@@ -721,7 +721,7 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
         for (int i = 0; i < 8; ++i) top = max(top, __float_as_uint(v[i]) & 0x7fffffffu);
 #pragma unroll
         for (int off = 1; off < HD / 8; off <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, off));
-        // 2^ex is at most the largest; below 2^-100 a row counts as 0
+        // 2^ex is at most the largest, and at least 2^-100 (below, a row has fewer bits)
         const int ex = max((int)(top >> 23) - 127, -100), to = F8 ? 10 : 21;
         const float f = __uint_as_float((uint32_t)(127 + to - ex) << 23);  // (ex 128: 2^-118 or 2^-107)
         if (d8 == 0) sm_c[row] = top >= 0x7f800000u ? __uint_as_float(0x7fc00000u) : scale2 * __uint_as_float((uint32_t)(127 - to + ex) << 23);
