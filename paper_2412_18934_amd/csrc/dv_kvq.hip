@@ -599,6 +599,17 @@ __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b)
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a), __builtin_bit_cast(u16x2, b)));
 }
 
+// Eight bf16, infinities and NaN as 0
+__device__ __forceinline__ u32x4 finite(u32x4 x)
+{
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if ((x[w] & 0x7f80u) == 0x7f80u) x[w] &= 0xffff0000u;
+        if ((x[w] & 0x7f800000u) == 0x7f800000u) x[w] &= 0xffffu;
+    }
+    return x;
+}
+
 __device__ __forceinline__ f32x4 mfma_bf16(const u32x4 &a, const u32x4 &b, const f32x4 &c)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -912,25 +923,45 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
         const bool odd = __any((top & 0xffffu) >= 0x7f80u || top >= 0x7f800000u);
         if (odd)
 #pragma unroll
-            for (int dt = 0; dt < ND; ++dt)
-#pragma unroll
-                for (int w = 0; w < 4; ++w) {
-                    if ((v[dt][w] & 0x7f80u) == 0x7f80u) v[dt][w] &= 0xffff0000u;
-                    if ((v[dt][w] & 0x7f800000u) == 0x7f800000u) v[dt][w] &= 0xffffu;
-                }
+            for (int dt = 0; dt < ND; ++dt) v[dt] = finite(v[dt]);
         // the sums' unit holds these numbers too (2^64: up to 2^128 they stay far from fp32's end)
         grow(__any((top & 0xffffu) >= 0x5f80u || top >= 0x5f800000u) ? 0x1p64f : 1.f);
         const float vs = v_inv * W_UNIT;
+        // Scores of part p of the queries.  A query's first part is 0 only where the query is, its
+        // others often: so infinities and NaN of K meet the first part only.
+        f32x4 sa_[RT], sb_[RT];
+        auto scores = [&](int p) {
+            each<RT>([&](auto rt_) {
+                constexpr int rt = decltype(rt_)::value;
+                if (row0 + 16 * rt >= rows) return;
+                if (p == 0) sa_[rt] = sb_[rt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < NC; ++c) {
+                    const u32x4 q = qt[rt][(3 * c + p) * 64 + lane];
+                    sa_[rt] = mfma_bf16(buf0.k[c], q, sa_[rt]);
+                    sb_[rt] = mfma_bf16(buf1.k[c], q, sb_[rt]);
+                }
+            });
+        };
+        scores(0);
+        top = 0;
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int w = 0; w < 4; ++w) top = max_u16x2(top, max_u16x2(buf0.k[c][w] & 0x7fff7fffu, buf1.k[c][w] & 0x7fff7fffu));
+        if (__any((top & 0xffffu) >= 0x7f80u || top >= 0x7f800000u)) {
+#pragma unroll
+            for (int c = 0; c < NC; ++c) {
+                buf0.k[c] = finite(buf0.k[c]);
+                buf1.k[c] = finite(buf1.k[c]);
+            }
+        }
+        scores(1);
+        scores(2);
         each<RT>([&](auto rt_) {
             constexpr int rt = decltype(rt_)::value;
             if (row0 + 16 * rt >= rows) return;
-            f32x4 sa = (f32x4){0.f, 0.f, 0.f, 0.f}, sb = sa;
-#pragma unroll
-            for (int c = 0; c < NT; ++c) {
-                const u32x4 q = qt[rt][c * 64 + lane];
-                sa = mfma_bf16(buf0.k[c / 3], q, sa);
-                sb = mfma_bf16(buf1.k[c / 3], q, sb);
-            }
+            const f32x4 sa = sa_[rt], sb = sb_[rt];
             // bit i: the row sees the lane's key i, committed or new row first + i
             const int first = s0 + 8 * g - a.r;
             const uint32_t see = (first >= 0 ? (uint32_t)(mask[rt] >> (first & 63))

@@ -1,0 +1,35 @@
+"""Attention over the 8-bit cache where rows that are seen hold infinities: a key whose score
+is -inf has no weight and takes nothing else with it, one whose score is +inf, or a
+value that is infinite or NaN, shows in every row that sees it."""
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("needs a GPU", allow_module_level=True)
+
+from tests.test_gpu_kvq import Pair, _check_attention, _rows  # noqa: E402
+
+
+@pytest.mark.parametrize("fmt,hd", [("i8", 64), ("f8", 64), ("i8", 128), ("f8", 128)])
+@pytest.mark.parametrize("len0,n,group", [(0, 6, 1), (40, 40, 1), (300, 9, 3), (300, 40, 1024)])
+def test_an_infinite_key(fmt, hd, len0, n, group):
+    """Queries of few bits and of many; in every third row the key's score is +inf."""
+    if group == 1024 and (fmt, hd) not in (("i8", 128), ("f8", 64)):
+        pytest.skip("32 rows a workgroup: two of the forms are enough")
+    rng = np.random.default_rng(len0 + n)
+    p = Pair(1, 1, hd, 32 * (len0 // 32 + 4), fmt)
+    p.preset(rng, len0)
+    new = {w: _rows(rng, (1, 1, n, hd)) for w in "kv"}
+    new["k"][0, 0, 2, 3], new["k"][0, 0, n - 1, hd - 1] = np.inf, -np.inf
+    q = rng.normal(0, 1.4, (n, group, hd))
+    q[::2] = np.round(q[::2] * 2) / 2                  # exact in the first of three parts
+    q[:, :, 3], q[:, :, hd - 1] = -1.5, 0.75
+    q[1::3, :, 3] = 2.0
+    with np.errstate(invalid="ignore"):
+        got, _ = _check_attention(p, rng, n, group, "chain", new=new, q=q.astype(np.float32).astype(np.float64))
+    seen = np.arange(n) >= 2
+    plus = np.arange(n) % 3 == 1
+    assert np.isfinite(got[~(seen & plus)]).all() and np.isnan(got[seen & plus]).all()
