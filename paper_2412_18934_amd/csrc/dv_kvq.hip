@@ -988,20 +988,21 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
 #pragma unroll
                 for (int p = 0; p < 3; ++p) o[rt][dt] = mfma_bf16(v[dt], p3[p], o[rt][dt]);
             if (!odd) return;
-            // an infinity or NaN counts for the rows that see its key, and is nothing (not
-            // 0 x infinity) for the others
+            // an infinity or NaN counts for the rows that see its key, however small its weight,
+            // and is nothing (not 0 x infinity) for the others
 #pragma unroll 1
             for (int key = 0; key < left; ++key) {
                 float p = w[0];
 #pragma unroll
                 for (int i = 1; i < 8; ++i) p = (key & 7) == i ? w[i] : p;
                 p = __shfl(p, 16 * (key >> 3) + n);
+                const bool seen = __shfl((int)see, 16 * (key >> 3) + n) >> (key & 7) & 1;
 #pragma unroll
                 for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
                         const float x = bf2f(vt[(dt * 16 + 4 * g + j) * 32 + key]);
-                        if (!__builtin_isfinite(x) && p != 0.f) o[rt][dt][j] += p * x;
+                        if (!__builtin_isfinite(x) && seen) o[rt][dt][j] += p * x;
                     }
             }
         });

@@ -33,3 +33,22 @@ def test_an_infinite_key(fmt, hd, len0, n, group):
     seen = np.arange(n) >= 2
     plus = np.arange(n) % 3 == 1
     assert np.isfinite(got[~(seen & plus)]).all() and np.isnan(got[seen & plus]).all()
+
+
+@pytest.mark.parametrize("fmt,hd,len0", [("i8", 64, 0), ("f8", 128, 50), ("i8", 128, 900)])
+def test_an_infinite_value_of_next_to_no_weight(fmt, hd, len0):
+    """A key so far below the others that its weight is no fp32 number: its infinity and NaN
+    show all the same, in the rows that see it and in their dims alone."""
+    rng = np.random.default_rng(hd)
+    n = 12
+    p = Pair(1, 2, hd, 32 * (len0 // 32 + 4), fmt)
+    p.preset(rng, len0)
+    new = {w: _rows(rng, (1, 2, n, hd), 1.0) for w in "kv"}
+    new["k"][0, :, 4] = -400 / np.sqrt(hd)             # about 400 nats below
+    new["v"][0, 0, 4, 7], new["v"][0, 1, 4, 9] = np.inf, np.nan
+    q = (1 + rng.normal(0, 0.05, (n, 2, hd))).astype(np.float32).astype(np.float64)
+    with np.errstate(invalid="ignore"):
+        got, _ = _check_attention(p, rng, n, 1, "chain", new=new, q=q)
+    want = np.ones((n, 2, hd), bool)
+    want[4:, 0, 7] = want[4:, 1, 9] = False
+    np.testing.assert_array_equal(np.isfinite(got), want)
