@@ -396,9 +396,11 @@ int64_t dv_kvq_attention_workspace(const dv_kvq *kvq, int32_t n, int32_t n_heads
  * cache (bf16 or int8 weights; n_layers, n_heads and head_dim are the model's).
  * Committed keys and values enter as scale * code, a step's or chain's own and the
  * tail's as bf16.  A prompt on the causal pass reads each layer back into one layer of
- * bf16 rows that the handle allocates at the first such prompt (4 d_model bytes per
- * slot), extends it there and appends the new rows; a chunk's own keys (up to 1024
- * tokens) enter as bf16.  Errors as theirs; DV_EINVAL too for fp32 weights or another
+ * bf16 rows, extends it there and appends the new rows; a chunk's own keys (up to 1024
+ * tokens) enter as bf16.  The handle allocates that layer (4 d_model bytes per slot) at
+ * the first such prompt, for twice the slots that the prompt ends at, or as many as
+ * capacity and max_ctx allow, and again when a prompt ends past it; without room for it
+ * the prompt runs as chains.  Errors as theirs; DV_EINVAL too for fp32 weights or another
  * model's cache, and a step is committed by the call of its own kind only
  * (DV_ESTATE). */
 int dv_verify_step_kvq(dv_handle *h, const int32_t *tokens, const int32_t *tree_parents, int32_t n_tree,

@@ -161,16 +161,24 @@ struct KvqSeam final : CacheSeam {
     int reserve(int slots) override
     {
         const int cap = (slots + 31) / 32 * 32;
-        const size_t one = (size_t)c->n_heads * cap * c->head_dim * 2;
+        const size_t slot = (size_t)c->n_heads * c->head_dim * 2, one = cap * slot;
         if (h->kvq_rows_bytes < 2 * one) {
+            // room for the turns behind this one too: every allocation and release of this size
+            // waits for the device
+            const int most = (std::min(c->capacity, h->cfg.max_ctx) + 31) / 32 * 32;
+            size_t bytes = 2 * slot * std::max(cap, (int)std::min<int64_t>(2ll * cap, most));
             void *p = nullptr;
-            if (hipMalloc(&p, 2 * one) != hipSuccess) {
+            if (hipMalloc(&p, bytes) != hipSuccess) {
                 (void)hipGetLastError();  // or the next launch would report it
-                return set_err(h, DV_ENOMEM, "no room for a layer of %d bf16 rows", cap);
+                bytes = 2 * one;
+                if (hipMalloc(&p, bytes) != hipSuccess) {
+                    (void)hipGetLastError();
+                    return set_err(h, DV_ENOMEM, "no room for a layer of %d bf16 rows", cap);
+                }
             }
             if (h->kvq_rows) (void)hipFree(h->kvq_rows);
             h->kvq_rows = p;
-            h->kvq_rows_bytes = 2 * one;
+            h->kvq_rows_bytes = bytes;
         }
         rows = {h->kvq_rows, static_cast<char *>(h->kvq_rows) + one, cap, 0};
         return DV_OK;

@@ -289,3 +289,32 @@ def test_handle_refusals(lib):
         assert lib.dv_prefill_kvq(e.h, dv._ptr(t), 4, ctypes.byref(cache()), None) == dv.DV_EINVAL
     finally:
         e.close()
+
+
+def test_a_growing_conversation_seldom_allocates(engine):
+    """The layer of bf16 rows is made for twice the prompt, as far as the cache goes: turns
+    behind it fit, and it grows a few times at most, not with every turn."""
+    def rows_made(n, fail_at=2 ** 64 - 1):
+        assert engine.prefill_kvq(n, fail_at) == 0
+        return [size for what, _, size in engine.log() if what == "malloc"]
+
+    slot = 2 * 4 * 64 * 2                              # K and V of 4 heads of 64
+    assert rows_made(300)[-1] == 640 * slot
+    for _ in range(3):
+        assert rows_made(100) == []                    # 600 slots
+    assert rows_made(100) == [1408 * slot]
+    made = 0
+    while engine.c.len < 4000:
+        made += len(rows_made(100))
+    assert made <= 2 and engine.c.len == 4000
+    # no room for twice: as much as the prompt needs, and nothing of the failure is left
+    engine.c.len = 0
+    other = KvqEngine(engine.lib, dv.DV_BF16)
+    try:
+        assert other.prefill_kvq(200) == 0             # (the pass's own workspace is there from here on)
+        other.c.len = 1200
+        assert other.prefill_kvq(200, fail_at=2000 * slot) == 0
+        assert [size for what, _, size in other.log() if what == "malloc"][-2:] == [2816 * slot, 1408 * slot]
+        assert other.log()[-1][0] == "sync" and "causal" in [what for what, _, _ in other.log()]
+    finally:
+        other.close()
