@@ -401,8 +401,8 @@ int64_t dv_kvq_attention_workspace(const dv_kvq *kvq, int32_t n, int32_t n_heads
  * the first such prompt, for twice the slots that the prompt ends at, or as many as
  * capacity and max_ctx allow, and again when a prompt ends past it; without room for it
  * the prompt runs as chains.  Errors as theirs; DV_EINVAL too for fp32 weights or another
- * model's cache, and a step is committed by the call of its own kind only
- * (DV_ESTATE). */
+ * model's cache, and a step is committed by the call of its own kind and on its own
+ * cache only: the same buffers, tails included, format, capacity and len (DV_ESTATE). */
 int dv_verify_step_kvq(dv_handle *h, const int32_t *tokens, const int32_t *tree_parents, int32_t n_tree,
                        dv_kvq *kvq, float *out_logits, dv_accept *out_accept);
 int dv_verify_step_kvq_sampled(dv_handle *h, const int32_t *tokens, const int32_t *tree_parents, int32_t n_tree,

@@ -93,7 +93,8 @@ struct dv_handle {
     int32_t pend_n = 0, pend_base = 0;
     int32_t pend_parents[DV_TREE_MAX];
     void *pend_k = nullptr, *pend_v = nullptr;
-    bool pend_kvq = false;  // of an 8-bit cache (its codes)
+    bool pend_kvq = false;  // of an 8-bit cache (its codes),
+    dv_kvq pend_cache{};    // which was this
 
     // prompts into an 8-bit cache: one layer's keys and values as bf16 (allocated at the
     // first such prompt)

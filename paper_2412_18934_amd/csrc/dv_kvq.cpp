@@ -200,6 +200,17 @@ int handle_view(dv_handle *h, const dv_kvq *c, dv_kv *view)
     return DV_OK;
 }
 
+int step(dv_handle *h, const int32_t *tokens, const int32_t *tree_parents, int32_t n_tree, dv_kvq *c, dv_kv *view,
+         float *out_logits, dv_accept *out_accept, const float *draft_probs, float temperature, const float *u_accept,
+         const float *u_bonus, bool sampled)
+{
+    KvqSeam seam(h, c);
+    const int rc = verify_step_impl(h, tokens, tree_parents, n_tree, view, out_logits, out_accept, draft_probs, temperature,
+                                    u_accept, u_bonus, sampled, &seam);
+    if (rc == DV_OK) h->pend_cache = *c;
+    return rc;
+}
+
 }  // namespace
 
 extern "C" {
@@ -313,9 +324,7 @@ int dv_verify_step_kvq(dv_handle *h, const int32_t *tokens, const int32_t *tree_
     dv_kv view;
     const int rc = handle_view(h, c, &view);
     if (rc) return rc;
-    KvqSeam seam(h, c);
-    return verify_step_impl(h, tokens, tree_parents, n_tree, &view, out_logits, out_accept, nullptr, 0.f, nullptr, nullptr,
-                            false, &seam);
+    return step(h, tokens, tree_parents, n_tree, c, &view, out_logits, out_accept, nullptr, 0.f, nullptr, nullptr, false);
 }
 
 int dv_verify_step_kvq_sampled(dv_handle *h, const int32_t *tokens, const int32_t *tree_parents, int32_t n_tree, dv_kvq *c,
@@ -325,9 +334,8 @@ int dv_verify_step_kvq_sampled(dv_handle *h, const int32_t *tokens, const int32_
     dv_kv view;
     const int rc = handle_view(h, c, &view);
     if (rc) return rc;
-    KvqSeam seam(h, c);
-    return verify_step_impl(h, tokens, tree_parents, n_tree, &view, out_logits, out_accept, draft_probs, temperature, u_accept,
-                            u_bonus, true, &seam);
+    return step(h, tokens, tree_parents, n_tree, c, &view, out_logits, out_accept, draft_probs, temperature, u_accept, u_bonus,
+                true);
 }
 
 int dv_prefill_kvq(dv_handle *h, const int32_t *tokens, int32_t n, dv_kvq *c, int32_t *out_next_token)
@@ -347,6 +355,9 @@ int dv_kvq_commit(dv_handle *h, dv_kvq *c, const dv_accept *acc)
     if (!acc) return set_err(h, DV_EINVAL, "null accept struct");
     bool identity;
     if ((rc = check_commit(h, &view, acc, true, &identity))) return rc;
+    // (caches may share blocks and have tails of their own, where the step's rows are)
+    if (std::memcmp(c, &h->pend_cache, sizeof *c))
+        return set_err(h, DV_ESTATE, "the cache is not the pending step's in all its buffers and sizes");
     const hipError_t e = launch_kvq_advance(layers_of(c, 0, c->n_layers), acc->path, acc->accept_len, h->stream);
     if (e != hipSuccess) return hip_fail(h, e, "cache advance launch");
     c->len += acc->accept_len;

@@ -318,3 +318,22 @@ def test_a_growing_conversation_seldom_allocates(engine):
         assert other.log()[-1][0] == "sync" and "causal" in [what for what, _, _ in other.log()]
     finally:
         other.close()
+
+
+def test_a_commit_takes_the_step_s_own_cache(engine):
+    """Caches may share blocks and differ in their tails, where a step's rows are; nor may
+    the shape that the rows were written with change."""
+    lib, c = engine.lib, engine.c
+    c.len = 61
+    t, p, acc = np.zeros(4, np.int32), np.array([-1, 0, 0, 2], np.int32), dv.dv_accept()
+    assert lib.dv_verify_step_kvq(engine.h, dv._ptr(t), dv._ptr(p), 4, ctypes.byref(c), None, ctypes.byref(acc)) == 0
+    acc.accept_len, acc.path[0], acc.path[1] = 2, 0, 2
+    lib.kvq_hush()
+    for other in (dict(k_tail=2 * A), dict(v_tail=2 * A), dict(scale=2 * A), dict(capacity=2048), dict(format=dv.DV_F8)):
+        o = cache(**{**dict(capacity=4096, len=61), **other})
+        assert lib.dv_kvq_commit(engine.h, ctypes.byref(o), ctypes.byref(acc)) == dv.DV_ESTATE and o.len == 61
+    assert engine.said() == []
+    # another struct of the same cache is the same cache
+    o = cache(capacity=4096, len=61)
+    assert lib.dv_kvq_commit(engine.h, ctypes.byref(o), ctypes.byref(acc)) == 0 and o.len == 63
+    assert engine.said() == [("advance", 61, 2, 2)]
