@@ -472,7 +472,9 @@ bool pf_supported(const dv_handle *h)
 // a fit to 260 prompts of 2 to 4 chains (d_model 256 to 6144, max_tree 1 to 64, 0
 // to 12000 cached keys).  Over those the choice is 0.5% behind the faster one on average,
 // 19% at most (58 against 68 us); without it the causal pass took up to 2.4 times as long as
-// the chains (d_model 1536, 10 tokens behind 7909 keys: 115 and 272 us a layer).
+// the chains (d_model 1536, 10 tokens behind 7909 keys: 115 and 272 us a layer).  Prompts
+// over an 8-bit cache take the same route, although their chains read fewer bytes and
+// their causal pass reads the cache back first: not fitted.
 bool chains_faster(const dv_handle *h, int n, int P0)
 {
     const dv_config &c = h->cfg;

@@ -38,19 +38,26 @@ hipError_t launch_kvq_advance(const KvqLayers &c, const int32_t *path, int n, hi
 
 // How a call's keys are cut: row tiles of up to 16 rt query rows (a KV head's n x
 // group rows) in z groups, n_split shares of the 32-key tiles.  A workgroup's 8 waves take
-// a tile each at a time, so z n_split heads is about the CUs.  Shares are dealt in groups
-// of 8 tiles in turn, so that the workgroups of a head read side by side: where each has
-// a range of its own, their distances can fall on the same memory channels (8 heads x 32
-// rows, 130001 slots: 61 to 66 us as ranges, by where the cache lies, 55 to 56 dealt).
+// a tile each at a time, and z n_split heads is as many of the CUs as whole shares make (129
+// of 256 at worst).  Shares are dealt in groups of 8 tiles in turn, so that the workgroups of
+// a head read side by side: where each has a range of its own, their distances can fall
+// on the same memory channels (8 heads x 32 rows, 130001 slots, weights in two parts: 61
+// to 66 us as ranges, by where the cache lies, 55 to 56 dealt).
 //
 // rt 2 reads and converts a tile once for 32 rows, rt 1 has twice the workgroups and no
-// waiting for the longer sums: 1 up to 12 tiles a wave.  us by tiles a wave, rt 1 / 2: 2.0
-// (8 heads x 32 rows, 8192 slots) 11.5 / 15.5, 5.2 (40 x 60, 2077) 15.1 / 18.1, 8.0 (8 x 64,
-// 16384) 18.6 / 20.5, 16 (32 x 32, 16384) 32.1 / 30.1, 32 (8 x 32, 130001) 58 / 55.
+// waiting for the longer sums: rt 1 up to 12 tiles a wave, counted as if rt 1 kept every CU
+// at work (one share of 129 to 255 workgroups has up to twice that).  us by that count,
+// rt 1 / 2, calls in a row:
+//   2.0 (8 heads x 32 rows, 8192 slots) 12.3 / 16.2     5.2 (40 x 60, 2077) 16.7 / 18.9
+//   8.0 (8 x 64, 16384) 20.2 / 21.4                     9.8 (40 x 60, 4000) 26.6 / 27.2
+//   12.0 (40 x 60, 4900) 28.9 / 26.9, int8 31.0 / 27.5  16 (32 x 32, 16384) 35.0 / 34.0
+//   32 (8 x 32, 130001) 72 / 60
+// (At 160 workgroups, the 40 x 60 ones, the better limit lies between 10 and 12.)
 //
 // Shares of less than 8 tiles leave waves idle, and several shares cost a second launch,
-// so up to 24 tiles stay one: 17 tiles of 32 heads 7.6 us as one share, 8.7 as three; 22 of 8
-// heads 8.8 and 8.7; 34 of 40 heads 10.3 and 10.0; 32 of 8 heads 9.9 and 8.6.
+// so up to 24 tiles stay one, us as one share and as several, calls in a row: 17 tiles of 32
+// heads 8.5 and 9.3; 22 of 8 heads 9.7 and 8.8; 34 of 40 heads 11.2 and 9.9; 32 of 8 heads
+// 11.1 and 8.8.  (In a step the second launch takes up to 1.7 us more.)
 struct KvqCut {
     int rt, z, n_split;
 };

@@ -513,12 +513,13 @@ template <bool F8, int HD> __global__ __launch_bounds__(256, 6) void k_kvq_advan
 // per row.  8 waves of a workgroup take tiles of their own, so no barrier stands between
 // tiles, and each asks for its next tile when the scores of the last row tile have used
 // K (V is converted by then): 64 KB per CU in flight while weights and sums are made.
-// Times, with the merge where there is one; in brackets what two tiles in flight, in two
-// sets of registers and twice the code, took more or less:
-//   8 heads x 32 rows, 130001 slots (267 MB)  53 to 55.5 us (+3), 4.9 TB/s; reading alone,
+// Times of calls in a row, with the merge where there is one; in brackets what two tiles in
+// flight, in two sets of registers and twice the code, took more or less (with weights in
+// two parts, as all that was not taken):
+//   8 heads x 32 rows, 130001 slots (267 MB)  57 to 61.5 us (+3), 4.5 TB/s; reading alone,
 //                                             this way cut, 41 to 45, and the merge 4.5
-//   32 heads x 1 row, 8191 slots (67 MB)      17.2 (+0.5): reading alone 12.4, merge
-//   40 heads x 60 rows, 2077 slots, e4m3      14.9 (+1): 160 workgroups, 9 tiles a wave
+//   32 heads x 1 row, 8191 slots (67 MB)      17.5 (+0.5): reading alone 12.4, merge
+//   40 heads x 60 rows, 2077 slots, e4m3      16.6 (+1): 160 workgroups, 9 tiles a wave
 //   40 heads x 16 rows, 1037 slots (12 MB)    9.5 (-0.1): latencies of 1 tile a wave, merge
 // Measured and not taken: 4 waves a workgroup (1 to 6 per CU), 12 and 16 waves per CU
 // (spills), 64 rows a workgroup, workgroups of a head on one XCD, a higher wave priority
@@ -1062,10 +1063,11 @@ template <int HD, bool F8, int RT, int NW> __global__ __launch_bounds__(64 * NW)
 
 // The shares combined, in a launch of its own: 4 threads share a row's 4 dims, each with
 // every fourth share, and are combined in LDS.  The order is fixed, so are the results.
-// 3 to 4.7 us, a launch's start and end and one chain of reads.  The last workgroup of a head
-// doing it in place of a launch was slower everywhere: it waits for its own writes and
-// for a counter, then merges alone (32 heads x 1 row, 8191 slots 18.7 us for 17.9; 8 x 32,
-// 130001 slots 67 for 58).
+// 3 to 4.7 us in a loop of calls, 4.7 to 4.9 in a step of a 13B model (16 nodes, 1037 slots),
+// a launch's start and end and one chain of reads.  The last workgroup of a head doing
+// it in place of a launch was slower everywhere: it waits for its own writes and for a
+// counter, then merges alone (32 heads x 1 row, 8191 slots 18.7 us for 17.9; 8 x 32, 130001
+// slots 67 for 58, at the time).
 template <int HD> __global__ __launch_bounds__(256) void k_kvq_merge(KvqOut a)
 {
     constexpr int D4 = HD / 4, NR = 64 / D4;  // rows of a workgroup

@@ -13,12 +13,14 @@ if not torch.cuda.is_available():
 from tests.test_gpu_kvq import Pair, _check_attention, _rows  # noqa: E402
 
 
-@pytest.mark.parametrize("fmt,hd", [("i8", 64), ("f8", 64), ("i8", 128), ("f8", 128)])
-@pytest.mark.parametrize("len0,n,group", [(0, 6, 1), (40, 40, 1), (300, 9, 3), (300, 40, 1024)])
+FORMS = [("i8", 64), ("f8", 64), ("i8", 128), ("f8", 128)]
+
+
+# (the last two: 32 rows a workgroup)
+@pytest.mark.parametrize("fmt,hd,len0,n,group", [(*f, *c) for c in ((0, 6, 1), (40, 40, 1), (300, 9, 3)) for f in FORMS] + [
+    ("i8", 128, 300, 40, 1024), ("f8", 64, 300, 40, 1024)])
 def test_an_infinite_key(fmt, hd, len0, n, group):
     """Queries of few bits and of many; in every third row the key's score is +inf."""
-    if group == 1024 and (fmt, hd) not in (("i8", 128), ("f8", 64)):
-        pytest.skip("32 rows a workgroup: two of the forms are enough")
     rng = np.random.default_rng(len0 + n)
     p = Pair(1, 1, hd, 32 * (len0 // 32 + 4), fmt)
     p.preset(rng, len0)
