@@ -10,7 +10,7 @@ torch = pytest.importorskip("torch")
 if not torch.cuda.is_available():
     pytest.skip("needs a GPU", allow_module_level=True)
 
-from tests.test_gpu_kvq import Pair, _check_attention, _rows  # noqa: E402
+from tests.test_gpu_kvq import Pair, _attend, _check_attention, _rows  # noqa: E402
 
 
 FORMS = [("i8", 64), ("f8", 64), ("i8", 128), ("f8", 128)]
@@ -54,3 +54,19 @@ def test_an_infinite_value_of_next_to_no_weight(fmt, hd, len0):
     want = np.ones((n, 2, hd), bool)
     want[4:, 0, 7] = want[4:, 1, 9] = False
     np.testing.assert_array_equal(np.isfinite(got), want)
+
+
+@pytest.mark.parametrize("fmt,hd", FORMS)
+def test_a_row_of_nothing_but_minus_infinity(fmt, hd):
+    """Zeros, as for a row that sees nothing; the rows that see more are not touched by it."""
+    rng = np.random.default_rng(3)
+    n = 5
+    p = Pair(1, 2, hd, 128, fmt)
+    new = {w: _rows(rng, (1, 2, n, hd), 1.0) for w in "kv"}
+    new["k"][0, :, 0, 1] = -np.inf
+    p.put(new, 0)
+    q = np.abs(rng.normal(0, 1, (n, 2, hd)))
+    got = _attend(p, q, n, 2, None)
+    assert not got[0].any()
+    want = _attend(p, q, n, 2, np.array([(2 << i) - 2 for i in range(n)], np.uint64))   # without key 0
+    np.testing.assert_array_equal(got, want)
