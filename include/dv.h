@@ -372,9 +372,10 @@ int dv_kvq_advance(dv_kvq *kvq, const int32_t *path, int32_t n, void *stream);
  *   out[i][h] = sum_j softmax_j(q[i][h] . k_j / sqrt(head_dim)) v_j
  * over the committed slots and the new rows j whose bit j of mask[i] is set
  * (dv_tree_prepare's out_anc; NULL: row i sees rows 0..i).  A row that sees nothing, or
- * nothing but scores of -infinity, gives zeros.  Scores, softmax and sums are fp32; against the committed blocks a query
- * is rounded first, by at most 2^-22 of its row's largest number (int8 codes), or 2^-23 of
- * itself and 2^-35 of its row's largest (e4m3), the largest counting as 2^-100 at least.
+ * nothing but scores of -infinity, gives zeros.  Scores, softmax and sums are fp32; against
+ * the committed blocks a query is rounded first, by at most 2^-22 of its row's largest
+ * number (int8 codes), or 2^-23 of itself and 2^-35 of its row's largest (e4m3), the
+ * largest counting as 2^-100 at least.
  *   q, out: device fp32 [n][n_heads][head_dim], rows q_stride and out_stride floats
  *     apart (multiples of 4, at least n_heads head_dim), 16-byte aligned.  n_heads is
  *     a multiple of kvq->n_heads, at most 1024 times as many: query heads h with the
