@@ -260,8 +260,6 @@ def _bound(s):
                                               c["interleaved"]))
         elif c["kind"] == "attend":
             ws = torch.empty(dv.dv_paged_attention_workspace(pg, rows), dtype=torch.uint8, device="cuda")
-        elif c["kind"] == "evict":
-            ws = torch.empty(dv.dv_paged_evict_workspace(pg), dtype=torch.uint8, device="cuda")
         s["bound"] = dv, pg, rows, rope, ws
     return s["bound"]
 
@@ -287,7 +285,7 @@ def _own(s):
         dv.dv_paged_commit(pg, s["path"].data_ptr(), s["path"].stride(0), s["path_len"].data_ptr(), s["new_lens"].data_ptr(),
                            stream)
     else:
-        dv.dv_paged_evict(pg, c["budget"], c["recent"], s["new_lens"].data_ptr(), ws.data_ptr(), ws.numel(), stream)
+        dv.dv_paged_evict(pg, c["budget"], c["recent"], s["new_lens"].data_ptr(), stream)
     return _whole(s)
 
 
