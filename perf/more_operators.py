@@ -367,7 +367,7 @@ def _append(s):
     x, nh, half = s["qkv"], c["heads"], c["rot"] // 2
     angle = s["positions"].double()[:, None] * s["freq"]
     cos, sin = ((f(angle) * _magnitude(c)).float()[:, None] for f in (torch.cos, torch.sin))
-    turned = x[:, :nh * (c["group"] + 1)].float()
+    turned = x[:, :nh * (c["group"] + 1)].to(torch.float32, copy=True)  # (keys are read only)
     if c["interleaved"]:
         a, b = turned[..., 0:c["rot"]:2], turned[..., 1:c["rot"]:2]
     else:
