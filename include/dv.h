@@ -412,6 +412,176 @@ int dv_verify_step_kvq_sampled(dv_handle *h, const int32_t *tokens, const int32_
 int dv_prefill_kvq(dv_handle *h, const int32_t *tokens, int32_t n, dv_kvq *kvq, int32_t *out_next_token);
 int dv_kvq_commit(dv_handle *h, dv_kvq *kvq, const dv_accept *accept);
 
+/* ---- paged KV cache of many sequences ------------------------------------
+ *
+ * The keys and values of many sequences in pages of a common pool, bf16.  A page is `page`
+ * slots of all layers and KV heads; a layer of a page is laid out as a layer of a dv_kv
+ * of that capacity (so pages are filled from a bf16 dv_kv, or copied back, by plain copies).
+ * Slot i of sequence s is slot i % page of page table[s][i / page].
+ *
+ *   k:     bf16 [n_layers][n_pages][n_heads][page][head_dim];
+ *   v:     bf16 [n_layers][n_pages][n_heads][page / 32][head_dim][32] (32-slot tiles, dim-major);
+ *   mass:  fp32 [n_layers][n_pages][n_heads][page], the attention weights that a slot got
+ *     (dv_paged_mass), or NULL where nothing is evicted;
+ *   table: int32 [n_seqs], rows of table_stride page numbers; entries behind a sequence's last slot
+ *     are not looked at;
+ *   lens:  int32 [n_seqs], committed slots of each sequence.
+ * All are DEVICE buffers of the caller (k, v and mass 16-byte aligned), read when the kernels
+ * run: a captured call follows the table and the lengths.  They need not start at zero.
+ * n_heads counts KV heads; head_dim is 64 or 128; page a multiple of 32; n_seqs at most 65536; a
+ * sequence has at most table_stride * page slots (2^30 at most); n_pages * n_heads * page is
+ * below 2^32.
+ *
+ * What stands in device memory is checked there.  A sequence whose numbers cannot be (a
+ * negative length, rows outside the call's, more slots than its table row has, a path that does not
+ * increase) is skipped: nothing of it is written.  A page number outside [0, n_pages) is a page
+ * that is not there: its slots are not seen, and what would be written to it is dropped.
+ * Either sets *fault (device int32, or NULL) to 1; nothing sets it back.
+ *
+ * Sequences may share pages that hold a common beginning: attention reads them, and
+ * dv_paged_append and dv_paged_commit write behind the committed slots only.  dv_paged_mass
+ * and dv_paged_evict write to all pages of a sequence: there a page stands in one place of the table
+ * only. */
+typedef struct dv_paged {
+    void *k;
+    void *v;
+    float *mass;
+    const int32_t *table;
+    int32_t *lens;
+    int32_t *fault;
+    int32_t n_layers;
+    int32_t n_heads;
+    int32_t head_dim;
+    int32_t n_pages;
+    int32_t page;
+    int32_t n_seqs;
+    int32_t table_stride;
+} dv_paged;
+
+/* The new rows of a call: every sequence's behind the other's.  New row i of sequence s is
+ * row start[s] + i; its slot is lens[s] + i.
+ *   q:     device [n_rows][n_heads][head_dim], DV_F32 or DV_BF16, rows q_stride elements apart
+ *     (rows of 16-byte alignment, at least n_heads head_dim).  n_heads is a multiple of the cache's,
+ *     at most 1024 times as many: query heads h with the same h / (n_heads / pg->n_heads) share
+ *     a KV head;
+ *   start: device int32 [n_seqs + 1], not decreasing; rows from start[n_seqs] on belong to nobody
+ *     and are left as they are.  NULL: one row per sequence, n_rows = n_seqs.  n_rows is at most 2^22;
+ *   mask:  device uint64 [n_rows]: bit j of a row: it sees new row j of its sequence (dv_tree_prepare's
+ *     out_anc).  NULL: new row i sees rows 0..i.  Committed slots are always seen;
+ *   scale: of the scores, 0 counts as 1 / sqrt(head_dim);  cap: scores z become cap tanh(z / cap), 0: not;
+ *   max_rows (1..64), max_len: about the most new rows of a sequence, and slots with
+ *     the new ones.  They choose how the work is cut; the results hold for any. */
+typedef struct dv_paged_rows {
+    void *q;
+    int64_t q_stride;
+    const int32_t *start;
+    const uint64_t *mask;
+    float scale;
+    float cap;
+    int32_t dtype;
+    int32_t n_heads;
+    int32_t n_rows;
+    int32_t max_rows;
+    int32_t max_len;
+} dv_paged_rows;
+
+/* Rotary positions.  Pair i of rot_dim / 2 is turned by position * freq[i]: dims 2 i and 2 i + 1
+ * (interleaved), or i and i + rot_dim / 2; dims from rot_dim on are not turned; cos and sin are
+ * multiplied by magnitude.  With f = base^(-2 i / rot_dim) and t = original_ctx f / (2 pi), the turns over
+ * the context that a model was trained on, freq[i] is
+ *   DV_ROPE_PLAIN      f;
+ *   DV_ROPE_LINEAR     f / factor;
+ *   DV_ROPE_TURNS      f (w + (1 - w) / factor), w = (t - low) / (high - low) in [0, 1]:
+ *                      pairs of many turns stay, those of few are stretched;
+ *   DV_ROPE_LOG_TURNS  the same with the logarithms of t, low and high.
+ * dv_rope_init checks the fields and fills freq (host only): rot_dim even and at most 128,
+ * base > 1, magnitude > 0; factor >= 1 unless plain; the last two: 0 < low < high and
+ * original_ctx > 0.  DV_EINVAL otherwise. */
+#define DV_ROPE_PLAIN 0
+#define DV_ROPE_LINEAR 1
+#define DV_ROPE_TURNS 2
+#define DV_ROPE_LOG_TURNS 3
+typedef struct dv_rope {
+    double base;
+    double factor;
+    double low;
+    double high;
+    double magnitude;
+    int32_t original_ctx;
+    int32_t scaling;
+    int32_t rot_dim;
+    int32_t interleaved;
+    double freq[64];
+} dv_rope;
+int dv_rope_init(dv_rope *rope);
+
+/* Operators on a paged cache.  Like those on an 8-bit cache they need no handle, allocate
+ * nothing, do not synchronise, and queue their kernels on `stream` (a hipStream_t of the current
+ * device, NULL = default stream), which may be capturing; structs are read during the call.
+ * Calls on one cache must be ordered where one writes what the other reads or writes.  Errors
+ * (message via dv_last_error(NULL)): DV_EINVAL, DV_EHIP. */
+
+/* The new rows' queries are turned in place, their keys turned and rounded to bf16 into their
+ * slots of layer `layer`, their values rounded to theirs, and the slots' mass is set to 0.  Any
+ * number of rows per sequence (a prompt's too).  The committed lengths do not change.
+ *   rows: q (or NULL: none), q_stride, start, dtype, n_heads, n_rows;
+ *   rope: as dv_rope_init left it, rot_dim at most head_dim, or NULL: nothing is turned;
+ *   positions: device int32 [n_rows], or NULL: the slots' numbers;
+ *   k, v: device [n_rows][pg->n_heads][head_dim] of rows->dtype, rows k_stride and v_stride elements
+ *     apart, aligned as q.  q, k and v may be parts of the same rows; their heads may not overlap. */
+int dv_paged_append(const dv_paged *pg, int32_t layer, const dv_paged_rows *rows, const dv_rope *rope,
+                    const int32_t *positions, const void *k, int64_t k_stride, const void *v, int64_t v_stride,
+                    void *stream);
+
+/* Attention of the new rows over layer `layer`, at most 64 per sequence (more: skipped as above):
+ *   out[r][h] = sum_j softmax_j(z_j) v_j,  z_j = scale q[r][h] . k_j, capped,
+ * over the committed slots and the new rows that the mask names.  A row that sees nothing, or nothing but
+ * scores of -infinity, gives zeros.  Products are exact (a DV_F32 query enters as three bf16
+ * parts), scores, softmax and sums fp32; weights enter with 24 bits (DV_F32) or 16 (DV_BF16, whose
+ * output has 8).  Slots that no row of the sequence sees may hold anything, NaN included, and so
+ * may new rows for those that do not see them.  Of what a row sees, a key whose score is -infinity has no
+ * weight, one whose score is +infinity or NaN makes the row NaN, and an infinity or NaN in a value makes
+ * the outputs of its dim infinite or NaN, however small its weight.
+ *   out:   device [n_rows][n_heads][head_dim] of rows->dtype, rows out_stride elements apart, aligned
+ *     as q; out may be q with the same stride; they may not overlap otherwise;
+ *   stats: device fp32 [n_rows][n_heads][2], or NULL: the largest z of a row and head, and
+ *     the sum of exp(z - largest) (nothing seen: -infinity and 0);
+ *   workspace: device memory, 16-byte aligned, of at least dv_paged_attention_workspace(pg, rows)
+ *     bytes (it may be 0, and workspace NULL).  Its contents do not matter before or after.  Calls
+ *     that may run at once, captured ones included, need one each. */
+int dv_paged_attention(const dv_paged *pg, int32_t layer, const dv_paged_rows *rows, void *out, int64_t out_stride,
+                       float *stats, void *workspace, int64_t workspace_bytes, void *stream);
+/* Bytes of workspace for these rows' n_heads, max_rows and max_len, or a negative error. */
+int64_t dv_paged_attention_workspace(const dv_paged *pg, const dv_paged_rows *rows);
+
+/* The weights of the new rows' attention are added to their slots' mass:
+ *   mass[slot][KV head] += sum over counted rows and the KV head's query heads of exp(z - stats[0]) / stats[1]
+ * with the queries, mask, scale and cap of the attention that wrote stats, before lens changes.
+ *   count: device uint64 [n_seqs], bit i: new row i counts (a tree's accepted path), or NULL: all do.
+ * Rows that do not count add nothing, whatever they hold.  The order of the sum is fixed. */
+int dv_paged_mass(const dv_paged *pg, int32_t layer, const dv_paged_rows *rows, const float *stats, const uint64_t *count,
+                  void *stream);
+
+/* New rows become committed, in all layers: new row path[s][i] moves to slot lens[s] + i, i <
+ * path_len[s], with its mass; other slots keep what they hold.
+ *   path: device int32 [n_seqs], rows of path_stride numbers, increasing, 0 <= path[s][i] < 64; or NULL:
+ *     rows 0..path_len - 1 stay where they are, any number of them;
+ *   path_len: device int32 [n_seqs], 0 and, with a path, 64 and path_stride at most;
+ *   new_lens: device int32 [n_seqs], set to lens + path_len (skipped sequences: lens); it
+ *     may be pg->lens, which costs a second launch, and may not overlap it otherwise. */
+int dv_paged_commit(const dv_paged *pg, const int32_t *path, int64_t path_stride, const int32_t *path_len,
+                    int32_t *new_lens, void *stream);
+
+/* Every sequence of more than `budget` committed slots is cut down to that: in each layer and KV head by itself
+ * the last `recent` slots stay, and of the others the budget - recent of largest mass, the
+ * lower slot of equal ones (a NaN is larger than all numbers, 0 and -0 are equal).  They move up to slots
+ * 0..budget - 1 in their order, with their mass; keys stay turned to the positions that they had.  Slots
+ * from budget on keep what they hold; their pages are free if nobody else has them.  Needs mass, 1 <=
+ * budget, 0 <= recent <= budget, table_stride * page at most 262144.
+ *   new_lens: device int32 [n_seqs], set to the smaller of lens and budget (skipped sequences:
+ *     lens); it may be pg->lens as above. */
+int dv_paged_evict(const dv_paged *pg, int32_t budget, int32_t recent, int32_t *new_lens, void *stream);
+
 /* Release the handle and its workspace (NULL is ignored). */
 void dv_verify_free(dv_handle *h);
 

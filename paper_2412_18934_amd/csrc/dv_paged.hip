@@ -1,0 +1,1091 @@
+// HIP kernels (gfx950) of the paged KV cache: rotary positions and the write of new rows,
+// attention over the pages, accumulated attention weights, commit and eviction.
+//
+// A (page, KV head, slot) has the row number (page H + head) page_slots + slot, below
+// 2^32: row r is K's elements r hd .. + hd, V's column r % 32 of the 32-slot tile
+// r / 32 (hd x 32, dim-major), and mass's element r.  A 32-slot tile of keys and its tile of
+// values start at the same element.
+#include <type_traits>
+
+#include "dv_device.h"
+#include "dv_paged_index.h"
+
+namespace {
+
+constexpr float LOG2E = 1.4426950408889634f;
+
+// ---------------------------------------------------------------------------
+// sequences, rows and shares
+
+__device__ __forceinline__ void report(const PagedView &c, bool bad)
+{
+    if (bad && c.fault) *c.fault = 1;  // (every writer writes the same)
+}
+
+// NT threads sum up all sequences' tiles, a run of sequences each.
+template <int NT> struct Line {
+    int64_t total, mine, sum;  // all tiles; those before this thread's sequences; theirs
+    int s0, s1;
+    template <typename W> __device__ __forceinline__ Line(int n_seqs, W w)
+    {
+        __shared__ int64_t sm_sum[NT / 64];
+        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+        const int per = (n_seqs + NT - 1) / NT;
+        s0 = min(tid * per, n_seqs);
+        s1 = min(s0 + per, n_seqs);
+        sum = 0;
+        for (int s = s0; s < s1; ++s) sum += w(s);
+        int64_t up = sum;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int64_t x = __shfl_up((long long)up, off);
+            if (lane >= off) up += x;
+        }
+        if (lane == 63) sm_sum[wave] = up;
+        __syncthreads();
+        mine = up - sum;
+        total = 0;
+#pragma unroll
+        for (int i = 0; i < NT / 64; ++i) {
+            if (i < wave) mine += sm_sum[i];
+            total += sm_sum[i];
+        }
+    }
+};
+
+// ---------------------------------------------------------------------------
+// conversions
+
+// Eight fp32 numbers as three bf16 each, by truncation: their sum is the number
+// (unless it is near the smallest ones).
+__device__ __forceinline__ void split3(const float *v, u32x4 (&t)[3])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint32_t w[3][2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            float x = v[2 * i + j];
+#pragma unroll
+            for (int p = 0; p < 3; ++p) {
+                w[p][j] = __float_as_uint(x);
+                x -= __uint_as_float(w[p][j] & 0xffff0000u);
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < 3; ++p) t[p][i] = __builtin_amdgcn_perm(w[p][1], w[p][0], 0x07060302u);
+    }
+}
+
+// As two bf16, the second to the nearest: off by at most 2^-17 of the number.
+__device__ __forceinline__ void split2(const float *v, u32x4 (&t)[2])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t a = __float_as_uint(v[2 * i]), b = __float_as_uint(v[2 * i + 1]);
+        t[0][i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        const bf16x2 low = {(__bf16)(v[2 * i] - __uint_as_float(a & 0xffff0000u)),
+                            (__bf16)(v[2 * i + 1] - __uint_as_float(b & 0xffff0000u))};
+        t[1][i] = __builtin_bit_cast(uint32_t, low);
+    }
+}
+
+// Eight bf16, infinities and NaN as 0
+__device__ __forceinline__ u32x4 finite(u32x4 x)
+{
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        if ((x[w] & 0x7f80u) == 0x7f80u) x[w] &= 0xffff0000u;
+        if ((x[w] & 0x7f800000u) == 0x7f800000u) x[w] &= 0xffffu;
+    }
+    return x;
+}
+
+__device__ __forceinline__ f32x4 mfma_bf16(const u32x4 &a, const u32x4 &b, const f32x4 &c)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+
+// Eight numbers of a row
+template <bool BF> __device__ __forceinline__ void load8(const void *p, int64_t at, float (&v)[8])
+{
+    if constexpr (BF) {
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(p) + at);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(i & 1 ? x[i >> 1] & 0xffff0000u : x[i >> 1] << 16);
+    } else {
+        const float *f = static_cast<const float *>(p) + at;
+        const float4 x = *reinterpret_cast<const float4 *>(f), y = *reinterpret_cast<const float4 *>(f + 4);
+        v[0] = x.x, v[1] = x.y, v[2] = x.z, v[3] = x.w, v[4] = y.x, v[5] = y.y, v[6] = y.z, v[7] = y.w;
+    }
+}
+__device__ __forceinline__ u32x4 bf16x8_of(const float (&v)[8])
+{
+    u32x4 x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = (uint32_t)f2bf(v[2 * i]) | (uint32_t)f2bf(v[2 * i + 1]) << 16;
+    return x;
+}
+template <bool BF> __device__ __forceinline__ void store8(void *p, int64_t at, const float (&v)[8])
+{
+    if constexpr (BF) {
+        *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(p) + at) = bf16x8_of(v);
+    } else {
+        float *f = static_cast<float *>(p) + at;
+        *reinterpret_cast<float4 *>(f) = make_float4(v[0], v[1], v[2], v[3]);
+        *reinterpret_cast<float4 *>(f + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    }
+}
+
+// f(0), .. f(N - 1) with constant arguments: a row tile's registers are never indexed
+template <int N, typename F> __device__ __forceinline__ void each(F f)
+{
+    if constexpr (N > 0) {
+        each<N - 1>(f);
+        f(std::integral_constant<int, N - 1>{});
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Append: x' = m (x cos - y sin), y' = m (y cos + x sin) for a pair (x, y) at angle position
+// * freq.  Angles are reduced in 64 bits (a position of 10^6 times a frequency of 1 leaves
+// fp32 seven bits behind the point); sin and cos are those of the angle's fp32 number with the
+// rest as a first-order term; products and sums are fp32, and a result is rounded once.
+
+// cos and sin of angle, times m
+__device__ __forceinline__ float2 turn_of(double angle, float m)
+{
+    const double k = rint(angle * 0.15915494309189535);  // whole turns; 2 pi in two parts
+    double r = fma(-k, 6.283185307179586, angle);
+    r = fma(-k, 2.4492935982947064e-16, r);
+    const float hi = (float)r, lo = (float)(r - hi);
+    float s, c;
+    sincosf(hi, &s, &c);
+    return make_float2(m * fmaf(-lo, s, c), m * fmaf(lo, c, s));
+}
+
+// The sequence that row `row` belongs to: how many of start[1 ..] are at most row.  All 64 lanes.
+__device__ __forceinline__ int seq_of_row(const int32_t *start, int n_seqs, int row)
+{
+    const int lane = threadIdx.x & 63;
+    int lo = 0, hi = n_seqs;
+    while (hi > lo) {
+        const int step = (hi - lo + 63) / 64, at = lo + (lane + 1) * step - 1;
+        const int below = __popcll(__ballot(at < hi && start[at + 1] <= row));
+        lo = min(lo + below * step, hi);
+        if (step == 1) break;
+        hi = min(hi, lo + step - 1);
+    }
+    return lo;
+}
+
+// Workgroup (row, group of heads): 8 dims of a head per thread.
+template <bool BF, int HD> __global__ __launch_bounds__(256) void k_paged_append(PagedAppendArgs a)
+{
+    constexpr int PER = HD / 8, HEADS = 256 / PER;
+    __shared__ float2 sm_turn[64];
+    __shared__ float sm_x[HEADS][HD];
+    const int row = blockIdx.x, tid = threadIdx.x, d0 = 8 * (tid % PER);
+    const int head = blockIdx.y * HEADS + tid / PER, kv = head - a.Hq, H = a.c.H;
+    const int s = a.start ? seq_of_row(a.start, a.c.n_seqs, row) : row;
+    if (s >= a.c.n_seqs) return;
+    bool bad = false;
+    const Seq q = seq_of(a.c, a.start, a.n_rows, s, 1 << 30, bad);
+    if (row < q.first || row - q.first >= q.n) {
+        report(a.c, bad);
+        return;
+    }
+    const int slot = q.len + row - q.first;
+    if (tid < a.rot / 2) sm_turn[tid] = turn_of((a.positions ? a.positions[row] : slot) * a.freq[tid], a.magnitude);
+    const bool there = head < a.Hq + 2 * H;
+    float x[8] = {};
+    if (there) {
+        const bool is_q = kv < 0, is_k = kv < H;
+        load8<BF>(is_q ? a.q : is_k ? a.k : a.v,
+                  row * (is_q ? a.ldq : is_k ? a.ldk : a.ldv) + (int64_t)(is_q ? head : is_k ? kv : kv - H) * HD + d0, x);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sm_x[tid / PER][d0 + i] = x[i];
+    }
+    __syncthreads();
+    if (!there) return;
+    if (kv < H) {
+        const int half = a.rot / 2;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int d = d0 + i;
+            if (d >= a.rot) break;
+            const bool second = a.interleaved ? d & 1 : d >= half;
+            const int pair = a.interleaved ? d >> 1 : second ? d - half : d;
+            const float y = sm_x[tid / PER][a.interleaved ? d ^ 1 : second ? d - half : d + half];
+            const float2 t = sm_turn[pair];
+            x[i] = fmaf(x[i], t.x, second ? y * t.y : -(y * t.y));
+        }
+        if (kv < 0) {
+            store8<BF>(a.q, row * a.ldq + (int64_t)head * HD + d0, x);
+            return;
+        }
+    }
+    const int h = kv < H ? kv : kv - H;
+    const uint32_t r = row_of(a.c, s, h, slot, bad);
+    report(a.c, bad);
+    if (r == NONE) return;
+    if (kv < H) {
+        *reinterpret_cast<u32x4 *>(a.c.k + (size_t)r * HD + d0) = bf16x8_of(x);
+        if (d0 == 0 && a.c.mass) a.c.mass[r] = 0.f;
+    } else {
+        uint16_t *to = a.c.v + ((size_t)(r / PAGED_TILE) * HD + d0) * PAGED_TILE + r % PAGED_TILE;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) to[i * PAGED_TILE] = f2bf(x[i]);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Attention of new rows over pages, split over the slots and joined.
+//
+//   z_ij = scale (q_i . k_j), capped: cap tanh(z / cap); over the slots that row i sees
+//   o_i = sum_j exp(z_ij - m_i) v_j / sum_j exp(z_ij - m_i), m_i the largest z: one pass,
+//   m and the sums rescaled when a larger z comes.
+//
+// Rows are a sequence's new tokens times the G query heads of a KV head, 16 rt to a block.
+//   S^T = K Q^T: A = 16 keys x dims, B = queries; the A rows of the two products of a tile
+//   are keys 8 (i / 4) + 4 t + i % 4, so D gives lane (n, g) the scores of row n for the keys
+//   8 g .. + 8, which are the B operand of O^T = V^T P^T; its D has 4 consecutive dims of
+//   row n.  A row's numbers belong to lanes n + 16 g, only its maximum crosses lanes.
+
+constexpr int NW = 8;  // waves of a workgroup
+
+// A 32-slot tile in registers, 16 bytes per lane and load
+template <int HD> struct Tile {
+    u32x4 k[HD / 16], v[HD / 16];
+    // (k: the two products' operands, HD / 32 each)
+    __device__ __forceinline__ void load_k(const uint16_t *base, uint32_t row, int lane)
+    {
+        const uint16_t *p = base + (size_t)row * HD + (8 * ((lane & 15) >> 2) + (lane & 3)) * HD + 8 * (lane >> 4);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int c = 0; c < HD / 32; ++c)
+                k[t * (HD / 32) + c] = *reinterpret_cast<const u32x4 *>(p + 4 * t * HD + 32 * c);
+    }
+    __device__ __forceinline__ void load_v(const uint16_t *base, uint32_t row, int lane)
+    {
+        const uint16_t *p = base + (size_t)row * HD + (lane & 15) * PAGED_TILE + 8 * (lane >> 4);
+#pragma unroll
+        for (int dt = 0; dt < HD / 16; ++dt) v[dt] = *reinterpret_cast<const u32x4 *>(p + dt * 16 * PAGED_TILE);
+    }
+};
+
+// Row numbers of a wave's next 64 tiles, lane i that of tile t + i step; NONE from `end` on.
+__device__ __forceinline__ uint32_t tile_rows(const PagedView &c, int s, int h, int t, int step, int end, int lane, bool &bad)
+{
+    const int64_t mine = t + (int64_t)lane * step;
+    return mine < end ? row_of(c, s, h, (int)mine * PAGED_TILE, bad) : NONE;
+}
+
+// Queries of a row block as B operands in LDS, NP parts: [rt][dims / 32][part][lane]
+template <int HD, bool BF, int RT>
+__device__ __forceinline__ void stage_queries(const PagedRowsView &r, const Seq &q, int h, int row0, u32x4 *to)
+{
+    constexpr int NP = BF ? 1 : 3, NC = HD / 32;
+    const int rows = q.n * r.G;
+    for (int e = threadIdx.x; e < RT * 16 * (HD / 8); e += 64 * NW) {
+        const int d8 = e % (HD / 8), row = e / (HD / 8), mine = row0 + row;
+        const int at = ((row / 16 * NC + (d8 >> 2)) * NP) * 64 + 16 * (d8 & 3) + row % 16;
+        const int64_t from = (int64_t)(q.first + mine / r.G) * r.ldq + ((int64_t)h * r.G + mine % r.G) * HD + 8 * d8;
+        if constexpr (BF) {
+            u32x4 x = {};
+            if (mine < rows) x = *reinterpret_cast<const u32x4 *>(static_cast<const uint16_t *>(r.q) + from);
+            to[at] = x;
+        } else {
+            float v[8] = {};
+            if (mine < rows) load8<false>(r.q, from, v);
+            u32x4 t[3];
+            split3(v, t);
+            bool odd = false;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) odd |= !__builtin_isfinite(v[i]);
+            if (odd) {  // an infinity or NaN is its first part, the others 0
+                t[0] = bf16x8_of(v);
+                t[1] = finite(t[1]);
+                t[2] = finite(t[2]);
+            }
+#pragma unroll
+            for (int p = 0; p < 3; ++p) to[at + p * 64] = t[p];
+        }
+    }
+}
+
+// Scores of a lane's 8 keys for the row tile at qs.  With a key's infinity the parts of a query that
+// are 0 (or of the other sign) make NaN of what is an infinity: where there is a NaN the infinities
+// and NaN of K meet the first part alone, which is 0 only where the query is.
+template <int HD, bool BF> __device__ __forceinline__ void scores8(const u32x4 *k, const u32x4 *qs, int lane, float (&s)[8])
+{
+    constexpr int NP = BF ? 1 : 3, NC = HD / 32;
+    f32x4 sa = {0.f, 0.f, 0.f, 0.f}, sb = sa;
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            const u32x4 q = qs[(c * NP + p) * 64 + lane];
+            sa = mfma_bf16(k[c], q, sa);
+            sb = mfma_bf16(k[NC + c], q, sb);
+        }
+    if constexpr (!BF) {
+        const float all = ((sa[0] + sa[1]) + (sa[2] + sa[3])) + ((sb[0] + sb[1]) + (sb[2] + sb[3]));
+        if (__any(all != all)) {
+            sa = sb = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                    const u32x4 q = qs[(c * NP + p) * 64 + lane];
+                    sa = mfma_bf16(p ? finite(k[c]) : k[c], q, sa);
+                    sb = mfma_bf16(p ? finite(k[NC + c]) : k[NC + c], q, sb);
+                }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = sa[i], s[4 + i] = sb[i];
+}
+
+__device__ __forceinline__ void scaled(const PagedRowsView &r, float (&s)[8])
+{
+    if (r.cap != 0.f) {
+        const float f = r.scale / r.cap;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] = r.cap * tanhf(s[i] * f);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[i] *= r.scale;
+    }
+}
+
+// Mask of a block row, and which of the lane's 8 keys from slot `slot` on it sees
+__device__ __forceinline__ uint64_t mask_of(const PagedRowsView &r, const Seq &q, int row)
+{
+    if (row >= q.n * r.G) return 0ull;
+    const int i = row / r.G;
+    return r.mask ? r.mask[q.first + i] : ~0ull >> (63 - i);
+}
+__device__ __forceinline__ uint32_t sees(uint64_t mask, const Seq &q, int slot)
+{
+    const int first = slot - q.len, mine = min(max(q.len + q.n - slot, 0), 8);
+    return (first >= 0 ? (uint32_t)(mask >> (first & 63))
+            : first > -8 ? (uint32_t)mask << -first | ((1u << -first) - 1) : 0xffu) & ((1u << mine) - 1);
+}
+
+template <bool BF> __device__ __forceinline__ void write_out(const PagedAttnArgs &a, int64_t at, const float (&o)[4])
+{
+    if constexpr (BF)
+        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + at) =
+            make_uint2((uint32_t)f2bf(o[0]) | (uint32_t)f2bf(o[1]) << 16, (uint32_t)f2bf(o[2]) | (uint32_t)f2bf(o[3]) << 16);
+    else
+        *reinterpret_cast<float4 *>(static_cast<float *>(a.out) + at) = make_float4(o[0], o[1], o[2], o[3]);
+}
+
+// A finished row: sums over the sum of weights, 0 if it saw nothing
+template <int HD, bool BF>
+__device__ __forceinline__ void finish(const PagedAttnArgs &a, const Seq &q, int h, int row, int d0, float m, float l, float (&o)[4])
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[j] = l == 0.f ? 0.f : o[j] / l;
+    const int64_t token = q.first + row / a.r.G, head = (int64_t)h * a.r.G + row % a.r.G;
+    write_out<BF>(a, token * a.ldo + head * HD + d0, o);
+    if (d0 == 0 && a.stats) a.stats[token * ((int64_t)a.c.H * a.r.G) + head] = make_float2(m, l);
+}
+
+template <int HD, bool BF, int RT, bool WHOLE> __global__ __launch_bounds__(64 * NW) void k_paged_attn(PagedAttnArgs a)
+{
+    constexpr int NC = HD / 32, ND = HD / 16, NP = BF ? 1 : 3, NV = BF ? 2 : 3;
+    constexpr int SUMS = NW * 16 * RT * (HD + 4) * 4, PARTS = RT * NC * NP * 1024;
+    __shared__ __align__(16) char sm[SUMS > PARTS ? SUMS : PARTS];  // queries, later the waves' sums
+    __shared__ float sm_m[NW][16 * RT], sm_l[NW][16 * RT];
+    __shared__ int64_t sm_before;
+    __shared__ int sm_s;
+    u32x4 *qs = reinterpret_cast<u32x4 *>(sm);
+    float(*sm_o)[16 * RT][HD + 4] = reinterpret_cast<float(*)[16 * RT][HD + 4]>(sm);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
+    bool bad = false;
+
+    // tiles [t0, t1) of row block b; slot: where partial sums go, below 0: these are all tiles
+    auto segment = [&](const Seq &q, int s, int h, int b, int t0, int t1, int slot) {
+        const int row0 = b * 16 * RT, rows = q.n * a.r.G;
+        const int plain = q.len / PAGED_TILE;  // tiles below: all slots committed
+        uint32_t ids = tile_rows(a.c, s, h, t0 + wave, NW, t1, lane, bad);
+        __syncthreads();
+        stage_queries<HD, BF, RT>(a.r, q, h, row0, qs);
+        uint64_t mask[RT];
+        float m_run[RT], l_run[RT];  // (l_run: of the lane's own keys)
+        f32x4 o[RT][ND];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            mask[rt] = t1 > plain ? mask_of(a.r, q, row0 + 16 * rt + n) : 0ull;
+            m_run[rt] = -INFINITY;
+            l_run[rt] = 0.f;
+#pragma unroll
+            for (int dt = 0; dt < ND; ++dt) o[rt][dt] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        }
+        Tile<HD> x;
+        int at = 0;
+        uint32_t row = __builtin_amdgcn_readlane(ids, 0);
+        // (loads never branch: where there is no tile they read the pool's first)
+        x.load_k(a.c.k, row == NONE ? 0 : row, lane);
+        x.load_v(a.c.v, row == NONE ? 0 : row, lane);
+        __syncthreads();
+        for (int t = t0 + wave; t < t1; t += NW) {
+            if (++at == 64) {
+                ids = tile_rows(a.c, s, h, t + NW, NW, t1, lane, bad);
+                at = 0;
+            }
+            const uint32_t next = __builtin_amdgcn_readlane(ids, at), from = next == NONE ? 0 : next;
+            const bool part = t >= plain;
+            float w[RT][8];
+            each<RT>([&](auto rt_) {
+                constexpr int rt = decltype(rt_)::value;
+                if (RT > 1 && row0 + 16 * rt >= rows) return;
+                scores8<HD, BF>(x.k, qs + rt * NC * NP * 64, lane, w[rt]);
+            });
+            x.load_k(a.c.k, from, lane);
+            bool odd = false;
+            uint32_t see[RT];
+            if (part) {
+                // V without the slots past the last row, which hold anything; infinities and NaN of
+                // new rows are taken out as well, and come after, for the rows that see them
+                const int mine = min(max(q.len + q.n - (t * PAGED_TILE + 8 * g), 0), 8);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) see[rt] = sees(mask[rt], q, t * PAGED_TILE + 8 * g);
+                bool any = false;
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        x.v[dt][i] &= (2 * i < mine ? 0xffffu : 0u) | (2 * i + 1 < mine ? 0xffff0000u : 0u);
+                        any |= (x.v[dt][i] & 0x7f80u) == 0x7f80u || (x.v[dt][i] & 0x7f800000u) == 0x7f800000u;
+                    }
+                odd = __any(any);
+                if (odd)
+#pragma unroll
+                    for (int dt = 0; dt < ND; ++dt) x.v[dt] = finite(x.v[dt]);
+            }
+            if (row != NONE)
+                each<RT>([&](auto rt_) {
+                    constexpr int rt = decltype(rt_)::value;
+                    if (RT > 1 && row0 + 16 * rt >= rows) return;
+                    float(&s8)[8] = w[rt];
+                    scaled(a.r, s8);
+                    if (part)
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) s8[i] = see[rt] >> i & 1 ? s8[i] : -INFINITY;
+                    float mt = s8[0];
+#pragma unroll
+                    for (int i = 1; i < 8; ++i) mt = fmaxf(mt, s8[i]);
+                    if (__any(mt > m_run[rt])) {
+                        mt = fmaxf(mt, __shfl_xor(mt, 16));
+                        mt = fmaxf(mt, __shfl_xor(mt, 32));
+                        const float mnew = fmaxf(m_run[rt], mt);
+                        const float alpha = m_run[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_run[rt] - mnew) * LOG2E);
+                        l_run[rt] *= alpha;
+#pragma unroll
+                        for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) o[rt][dt][j] *= alpha;
+                        m_run[rt] = mnew;
+                    }
+                    float ps = 0.f;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        s8[i] = s8[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((s8[i] - m_run[rt]) * LOG2E);
+                        ps += s8[i];
+                    }
+                    l_run[rt] += ps;
+                    u32x4 p[NV];
+                    if constexpr (BF)
+                        split2(s8, p);
+                    else
+                        split3(s8, p);
+#pragma unroll
+                    for (int i = 0; i < NV; ++i)
+#pragma unroll
+                        for (int dt = 0; dt < ND; ++dt) o[rt][dt] = mfma_bf16(x.v[dt], p[i], o[rt][dt]);
+                    if (!odd) return;
+                    // an infinity or NaN counts for the rows that see its key, however small its weight
+                    const uint16_t *vt = a.c.v + (size_t)row * HD;
+                    const int left = min(PAGED_TILE, q.len + q.n - t * PAGED_TILE);
+#pragma unroll 1
+                    for (int key = 0; key < left; ++key) {
+                        float pk = s8[0];
+#pragma unroll
+                        for (int i = 1; i < 8; ++i) pk = (key & 7) == i ? s8[i] : pk;
+                        pk = __shfl(pk, 16 * (key >> 3) + n);
+                        const bool seen = __shfl((int)see[rt], 16 * (key >> 3) + n) >> (key & 7) & 1;
+#pragma unroll
+                        for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) {
+                                const float y = bf2f(vt[(dt * 16 + 4 * g + j) * PAGED_TILE + key]);
+                                if (!__builtin_isfinite(y) && seen) o[rt][dt][j] += pk * y;
+                            }
+                    }
+                });
+            x.load_v(a.c.v, from, lane);
+            row = next;
+        }
+
+        // combine the waves, in their order
+        const int rows_here = min(16 * RT, rows - row0), active = min(NW, t1 - t0);
+        __syncthreads();
+        if (wave < active)
+            each<RT>([&](auto rt_) {
+                constexpr int rt = decltype(rt_)::value;
+                float l = l_run[rt];
+                l += __shfl_xor(l, 16);
+                l += __shfl_xor(l, 32);
+                if (16 * rt + n >= rows_here) return;
+                if (g == 0) {
+                    sm_m[wave][16 * rt + n] = m_run[rt];
+                    sm_l[wave][16 * rt + n] = l;
+                }
+#pragma unroll
+                for (int dt = 0; dt < ND; ++dt)
+                    *reinterpret_cast<f32x4 *>(&sm_o[wave][16 * rt + n][dt * 16 + 4 * g]) = o[rt][dt];
+            });
+        __syncthreads();
+        for (int e = tid; e < rows_here * (HD / 4); e += 64 * NW) {
+            const int i = e / (HD / 4), d0 = 4 * (e % (HD / 4));
+            float m = -INFINITY, l = 0.f, ov[4] = {0.f, 0.f, 0.f, 0.f};
+            for (int w = 0; w < active; ++w) m = fmaxf(m, sm_m[w][i]);
+            for (int w = 0; w < active; ++w) {
+                const float mw = sm_m[w][i], f = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mw - m) * LOG2E);
+                // (a wave whose every score is NaN has a largest of -infinity and a sum of NaN)
+                l += mw == -INFINITY ? sm_l[w][i] : f * sm_l[w][i];
+                const f32x4 o4 = *reinterpret_cast<const f32x4 *>(&sm_o[w][i][d0]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) ov[j] = mw == -INFINITY ? ov[j] + o4[j] : fmaf(f, o4[j], ov[j]);
+            }
+            if (slot < 0) {
+                finish<HD, BF>(a, q, h, row0 + i, d0, m, l, ov);
+            } else {
+                const int64_t p = (int64_t)slot * 16 * RT + i;
+                *reinterpret_cast<float4 *>(a.part_o + p * HD + d0) = make_float4(ov[0], ov[1], ov[2], ov[3]);
+                if (d0 == 0) a.part_ml[p] = make_float2(m, l);
+            }
+        }
+    };
+
+    if constexpr (WHOLE) {
+        const int s = blockIdx.x / a.c.H, h = blockIdx.x % a.c.H;
+        const Seq q = seq_of(a.c, a.r.start, a.r.n_rows, s, PAGED_MAX_NEW, bad);
+        const Load w = load_of(a.c, q, a.r.G, 16 * RT);
+        for (int b = blockIdx.y; b < w.units / a.c.H; b += gridDim.y) segment(q, s, h, b, 0, w.tiles, -1);
+    } else {
+        const int me = blockIdx.x;
+        auto weight = [&](int s) {
+            const Load w = load_of(a.c, seq_of(a.c, a.r.start, a.r.n_rows, s, PAGED_MAX_NEW, bad), a.r.G, 16 * RT);
+            return (int64_t)w.units * w.tiles;
+        };
+        const Line<64 * NW> line(a.c.n_seqs, weight);
+        const int groups = shares_of(line.total, a.groups);
+        int64_t at = me < groups ? share_start(line.total, me, groups) : 0;
+        const int64_t end = me < groups ? share_start(line.total, me + 1, groups) : 0;
+        if (at < end) {  // (the same in all threads)
+            if (at >= line.mine && at < line.mine + line.sum) {
+                int64_t before = line.mine;
+                for (int s = line.s0; s < line.s1; ++s) {
+                    const int64_t w = weight(s);
+                    if (at < before + w) {
+                        sm_s = s;
+                        sm_before = before;
+                        break;
+                    }
+                    before += w;
+                }
+            }
+            __syncthreads();
+            int64_t before = sm_before;
+            for (int s = sm_s; at < end && s < a.c.n_seqs; ++s) {
+                const Seq q = seq_of(a.c, a.r.start, a.r.n_rows, s, PAGED_MAX_NEW, bad);
+                const Load w = load_of(a.c, q, a.r.G, 16 * RT);
+                const int64_t all = (int64_t)w.units * w.tiles;
+                while (at < end && at < before + all) {
+                    const int unit = (int)((at - before) / w.tiles), t0 = (int)((at - before) % w.tiles);
+                    const int t1 = (int)min((int64_t)w.tiles, t0 + (end - at)), blocks = w.units / a.c.H;
+                    segment(q, s, unit / blocks, unit % blocks, t0, t1,
+                            t0 == 0 && t1 == w.tiles ? -1 : 2 * me + (t0 == 0));
+                    at += t1 - t0;
+                }
+                before += all;
+            }
+        }
+    }
+    report(a.c, bad);
+}
+
+// The shares of a row block combined, in their order, in a launch of its own.  Workgroup
+// (sequence and KV head, rows): HD / 4 threads have 4 dims of a row each.
+template <int HD, bool BF, int RT> __global__ __launch_bounds__(256) void k_paged_merge(PagedAttnArgs a)
+{
+    __shared__ int64_t sm_before;
+    constexpr int PER = HD / 4, AT_ONCE = 256 / PER;
+    const int tid = threadIdx.x, s = blockIdx.x / a.c.H, h = blockIdx.x % a.c.H, d0 = 4 * (tid % PER);
+    bool bad = false;
+    auto weight = [&](int i) {
+        const Load w = load_of(a.c, seq_of(a.c, a.r.start, a.r.n_rows, i, PAGED_MAX_NEW, bad), a.r.G, 16 * RT);
+        return (int64_t)w.units * w.tiles;
+    };
+    const Line<256> line(a.c.n_seqs, weight);
+    if (s >= line.s0 && s < line.s1) {
+        int64_t before = line.mine;
+        for (int i = line.s0; i < s; ++i) before += weight(i);
+        sm_before = before;
+    }
+    __syncthreads();
+    const Seq q = seq_of(a.c, a.r.start, a.r.n_rows, s, PAGED_MAX_NEW, bad);
+    const Load w = load_of(a.c, q, a.r.G, 16 * RT);
+    const int rows = q.n * a.r.G, blocks = w.units / a.c.H, groups = shares_of(line.total, a.groups);
+    for (int row = blockIdx.y * AT_ONCE + tid / PER; row < rows; row += gridDim.y * AT_ONCE) {
+        const int b = row / (16 * RT), i = row % (16 * RT);
+        const int64_t first = sm_before + ((int64_t)h * blocks + b) * w.tiles, last = first + w.tiles - 1;
+        const int g0 = share_of(line.total, first, groups), g1 = share_of(line.total, last, groups);
+        if (g0 == g1) continue;  // (one workgroup had it all)
+        float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int g = g0; g <= g1; ++g) m = fmaxf(m, a.part_ml[(int64_t)(2 * g + (g == g0)) * 16 * RT + i].x);
+        for (int g = g0; g <= g1; ++g) {
+            const int64_t p = (int64_t)(2 * g + (g == g0)) * 16 * RT + i;
+            const float2 ml = a.part_ml[p];
+            const float f = ml.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((ml.x - m) * LOG2E);
+            const float4 x = *reinterpret_cast<const float4 *>(a.part_o + p * HD + d0);
+            l = fmaf(f, ml.y, l);
+            o[0] = fmaf(f, x.x, o[0]);
+            o[1] = fmaf(f, x.y, o[1]);
+            o[2] = fmaf(f, x.z, o[2]);
+            o[3] = fmaf(f, x.w, o[3]);
+        }
+        finish<HD, BF>(a, q, h, row, d0, m, l, o);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Mass: mass_j += sum over counted rows of exp(z_ij - m_i) / l_i.  The scores are made again
+// from K alone, half of what attention read; a tile belongs to one wave, which adds its
+// rows in order, so nothing is atomic.
+
+template <int HD, bool BF> __global__ __launch_bounds__(64 * NW) void k_paged_mass(PagedMassArgs a)
+{
+    constexpr int NC = HD / 32, NP = BF ? 1 : 3, RT = 4;  // row tiles at a time
+    __shared__ __align__(16) u32x4 qs[RT * NC * NP * 64];
+    __shared__ int64_t sm_before;
+    __shared__ int sm_s;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
+    bool bad = false;
+
+    auto segment = [&](const Seq &q, int s, int h, int t0, int t1) {
+        const int rows = q.n * a.r.G, plain = q.len / PAGED_TILE;
+        const uint64_t count = a.count ? a.count[s] : ~0ull;
+        for (int row0 = 0; row0 < rows; row0 += 16 * RT) {
+            uint32_t ids = tile_rows(a.c, s, h, t0 + wave, NW, t1, lane, bad);
+            __syncthreads();
+            stage_queries<HD, BF, RT>(a.r, q, h, row0, qs);
+            uint64_t mask[RT];
+            float m[RT], f[RT];  // a row that does not count: f < 0
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const int row = row0 + 16 * rt + n, i = row / a.r.G;
+                mask[rt] = mask_of(a.r, q, row);
+                m[rt] = 0.f;
+                f[rt] = -1.f;
+                if (row < rows && count >> i & 1) {
+                    const float2 ml = a.stats[(int64_t)(q.first + i) * ((int64_t)a.c.H * a.r.G) + (int64_t)h * a.r.G + row % a.r.G];
+                    m[rt] = ml.x;
+                    if (ml.y != 0.f) f[rt] = 1.f / ml.y;
+                }
+            }
+            Tile<HD> x;
+            int at = 0;
+            uint32_t row = __builtin_amdgcn_readlane(ids, 0);
+            x.load_k(a.c.k, row == NONE ? 0 : row, lane);
+            __syncthreads();
+            for (int t = t0 + wave; t < t1; t += NW) {
+                if (++at == 64) {
+                    ids = tile_rows(a.c, s, h, t + NW, NW, t1, lane, bad);
+                    at = 0;
+                }
+                const uint32_t next = __builtin_amdgcn_readlane(ids, at);
+                float sum[8] = {};
+                each<RT>([&](auto rt_) {
+                    constexpr int rt = decltype(rt_)::value;
+                    if (row0 + 16 * rt >= rows) return;
+                    float z[8];
+                    scores8<HD, BF>(x.k, qs + rt * NC * NP * 64, lane, z);
+                    scaled(a.r, z);
+                    const uint32_t see = t < plain ? 0xffu : sees(mask[rt], q, t * PAGED_TILE + 8 * g);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        const float w = __builtin_amdgcn_exp2f((z[i] - m[rt]) * LOG2E) * f[rt];
+                        // (f of a NaN sum is NaN, and shows)
+                        sum[i] += (see >> i & 1) && !(f[rt] < 0.f) ? w : 0.f;
+                    }
+                });
+                x.load_k(a.c.k, next == NONE ? 0 : next, lane);
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int off = 1; off < 16; off <<= 1) sum[i] += __shfl_xor(sum[i], off);
+                if (row != NONE && n == 0) {
+                    float *to = a.c.mass + (size_t)row + 8 * g;
+                    const int mine = min(max(q.len + q.n - (t * PAGED_TILE + 8 * g), 0), 8);
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (i < mine) to[i] += sum[i];
+                }
+                row = next;
+            }
+        }
+    };
+
+    auto weight = [&](int s) {
+        const Load w = load_of(a.c, seq_of(a.c, a.r.start, a.r.n_rows, s, PAGED_MAX_NEW, bad), a.r.G, 1 << 30);
+        return (int64_t)w.units * w.tiles;
+    };
+    const Line<64 * NW> line(a.c.n_seqs, weight);
+    int64_t at = share_start(line.total, blockIdx.x, gridDim.x);
+    const int64_t end = share_start(line.total, blockIdx.x + 1, gridDim.x);
+    if (at < end) {
+        if (at >= line.mine && at < line.mine + line.sum) {
+            int64_t before = line.mine;
+            for (int s = line.s0; s < line.s1; ++s) {
+                const int64_t w = weight(s);
+                if (at < before + w) {
+                    sm_s = s;
+                    sm_before = before;
+                    break;
+                }
+                before += w;
+            }
+        }
+        __syncthreads();
+        int64_t before = sm_before;
+        for (int s = sm_s; at < end && s < a.c.n_seqs; ++s) {
+            const Seq q = seq_of(a.c, a.r.start, a.r.n_rows, s, PAGED_MAX_NEW, bad);
+            const Load w = load_of(a.c, q, a.r.G, 1 << 30);
+            const int64_t all = (int64_t)w.units * w.tiles;
+            while (at < end && at < before + all) {
+                const int h = (int)((at - before) / w.tiles), t0 = (int)((at - before) % w.tiles);
+                const int t1 = (int)min((int64_t)w.tiles, t0 + (end - at));
+                segment(q, s, h, t0, t1);
+                at += t1 - t0;
+            }
+            before += all;
+        }
+    }
+    report(a.c, bad);
+}
+
+// ---------------------------------------------------------------------------
+// Commit and eviction move rows of a (layer, sequence, KV head) to lower slots, in order.
+// Source slots increase, and each is at least its destination; so a wave that always
+// has the same columns of K (or dims of V) can go through the list by itself: what it
+// overwrites is no later row's source, and a step's loads stand before its stores.
+
+constexpr int MOVE = 1024;  // rows of a list
+
+// Rows list[i].x to list[i].y, i < count; NONE in either: not moved.  8 waves.
+template <int HD> __device__ __forceinline__ void move_rows(const PagedView &c, int layer, const uint2 *list, int count)
+{
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const size_t base = (size_t)layer * c.n_pages * c.H * c.page;
+    if (wave < 4) {  // K: a quarter of the columns
+        constexpr int CH = HD / 32, ROWS = 64 / CH, U = 4;  // 16 bytes each
+        uint16_t *k = c.k + base * HD + (wave * CH + lane % CH) * 8;
+        for (int i0 = 0; i0 < count; i0 += ROWS * U) {
+            u32x4 x[U];
+            uint2 at[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int i = i0 + u * ROWS + lane / CH;
+                at[u] = i < count ? list[i] : make_uint2(NONE, NONE);
+                if (at[u].x == NONE || at[u].y == NONE) at[u].y = NONE;
+                else x[u] = *reinterpret_cast<const u32x4 *>(k + (size_t)at[u].x * HD);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (at[u].y != NONE) *reinterpret_cast<u32x4 *>(k + (size_t)at[u].y * HD) = x[u];
+        }
+        if (wave == 0 && c.mass) {
+            float *mass = c.mass + base;
+            for (int i = lane; i < count; i += 64) {
+                const uint2 e = list[i];
+                if (e.x == NONE || e.y == NONE) continue;
+                const float m = mass[e.x];
+                mass[e.y] = m;
+            }
+        }
+    } else {  // V: a quarter of the dims, 32 rows at a time, two dims a load
+        constexpr int U = HD / 8;
+        uint16_t *v = c.v + base * HD + ((wave - 4) * (HD / 4) + lane / 32) * PAGED_TILE;
+        for (int i0 = 0; i0 < count; i0 += 32) {
+            const int i = i0 + lane % 32;
+            uint2 e = i < count ? list[i] : make_uint2(NONE, NONE);
+            const bool moves = e.x != NONE && e.y != NONE;
+            uint16_t x[U];
+            const uint16_t *from = v + (size_t)(e.x / PAGED_TILE) * HD * PAGED_TILE + e.x % PAGED_TILE;
+            uint16_t *to = v + (size_t)(e.y / PAGED_TILE) * HD * PAGED_TILE + e.y % PAGED_TILE;
+            if (moves) {
+#pragma unroll
+                for (int u = 0; u < U; ++u) x[u] = from[2 * u * PAGED_TILE];
+#pragma unroll
+                for (int u = 0; u < U; ++u) to[2 * u * PAGED_TILE] = x[u];
+            }
+        }
+    }
+}
+
+template <int HD> __global__ __launch_bounds__(512) void k_paged_commit(PagedMoveArgs a)
+{
+    __shared__ uint2 list[PAGED_MAX_NEW];
+    const int h = blockIdx.x % a.c.H, s = blockIdx.x / a.c.H % a.c.n_seqs, layer = blockIdx.x / a.c.H / a.c.n_seqs;
+    const int len = a.c.lens[s], n = a.path_len[s], i = threadIdx.x;
+    const bool first = h == 0 && layer == 0 && i == 0, apart = a.new_lens != a.c.lens;
+    const bool fits = commit_fits(a, s);
+    if (__syncthreads_or(!fits || (i < n && !path_ok(a, s, i, n)))) {
+        if (first) report(a.c, true);
+        if (first && apart) a.new_lens[s] = len;
+        return;
+    }
+    if (first && apart) a.new_lens[s] = len + n;
+    bool bad = false;
+    if (i < n) {
+        const int from = a.path[s * a.path_stride + i];
+        list[i] = from == i ? make_uint2(NONE, NONE)
+                            : make_uint2(row_of(a.c, s, h, len + from, bad), row_of(a.c, s, h, len + i, bad));
+    }
+    __syncthreads();
+    report(a.c, bad);
+    move_rows<HD>(a.c, layer, list, n);
+}
+
+__global__ __launch_bounds__(256) void k_paged_commit_lens(PagedMoveArgs a)
+{
+    const int s = blockIdx.x * 256 + threadIdx.x;
+    if (s >= a.c.n_seqs) return;
+    const int len = a.c.lens[s], n = a.path_len[s];
+    bool ok = commit_fits(a, s);
+    if (a.path)
+        for (int i = 0; ok && i < n; ++i) ok = path_ok(a, s, i, n);
+    report(a.c, !ok);
+    a.new_lens[s] = ok ? len + n : len;
+}
+
+// ---------------------------------------------------------------------------
+// Eviction, a workgroup for each (layer, sequence, KV head): the mass that separates what stays
+// is found digit by digit from the top, counted in LDS; then every slot's bit is made (equal
+// masses: the lower slots), and the slots whose bit is set move up.
+
+template <int HD> __global__ __launch_bounds__(512) void k_paged_evict(PagedMoveArgs a)
+{
+    constexpr int NT = 512, BITS = 11, BINS = 1 << BITS;
+    extern __shared__ uint32_t sm_bits[];
+    __shared__ uint32_t hist[BINS];
+    __shared__ uint2 list[MOVE];
+    __shared__ uint32_t sm_wave[NT / 64], sm_bin, sm_above, sm_word[MOVE / 32 + 1];
+    const int h = blockIdx.x % a.c.H, s = blockIdx.x / a.c.H % a.c.n_seqs, layer = blockIdx.x / a.c.H / a.c.n_seqs;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, N = a.c.lens[s];
+    const bool first = h == 0 && layer == 0 && tid == 0, apart = a.new_lens != a.c.lens;
+    if (N < 0 || N > (int64_t)a.c.width * a.c.page || N <= a.budget) {
+        if (first) report(a.c, N < 0 || N > (int64_t)a.c.width * a.c.page);
+        if (first && apart) a.new_lens[s] = N;
+        return;
+    }
+    if (first && apart) a.new_lens[s] = a.budget;
+    bool bad = false;
+    const int M = N - a.recent, keep = a.budget - a.recent;  // keep < M
+    const float *mass = a.c.mass + (size_t)layer * a.c.n_pages * a.c.H * a.c.page;
+    auto rank = [&](int slot) {
+        const uint32_t r = row_of(a.c, s, h, slot, bad);
+        return r == NONE ? 0u : rank_of(mass[r]);
+    };
+
+    // the keep-th largest rank, and how many of that rank stay
+    uint32_t want = 0, left = keep;
+    if (keep > 0) {
+#pragma unroll 1
+        for (int shift = 21; shift >= 0; shift -= shift > 10 ? 11 : 10) {
+            // digits: bits 31..21, 20..10, 9..0
+            const uint32_t mask = shift == 0 ? 0x3ffu : 0x7ffu, above = shift == 21 ? 0u : shift == 10 ? 0xffe00000u : 0xfffffc00u;
+            for (int i = tid; i < BINS; i += NT) hist[i] = 0;
+            __syncthreads();
+            for (int i = tid; i < M; i += NT) {
+                const uint32_t r = rank(i);
+                if ((r & above) == want) atomicAdd(&hist[r >> shift & mask], 1u);
+            }
+            __syncthreads();
+            // bins from the top, 4 a thread: the one where the count reaches `left`
+            uint32_t c[4], sum = 0;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum += c[i] = hist[BINS - 1 - 4 * tid - i];
+            uint32_t up = sum;
+#pragma unroll
+            for (int off = 1; off < 64; off <<= 1) {
+                const uint32_t x = __shfl_up(up, off);
+                if (lane >= off) up += x;
+            }
+            if (lane == 63) sm_wave[wave] = up;
+            __syncthreads();
+            uint32_t before = up - sum;
+            for (int i = 0; i < wave; ++i) before += sm_wave[i];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (before < left && left <= before + c[i]) {
+                    sm_bin = BINS - 1 - 4 * tid - i;
+                    sm_above = before;
+                }
+                before += c[i];
+            }
+            __syncthreads();
+            want |= sm_bin << shift;
+            left -= sm_above;
+        }
+    }
+    // `left` slots of rank `want` stay (the lowest); each wave has a run of slots
+    const int run = (N + NT - 1) / NT * 64, lo = min(wave * run, N), hi = min(lo + run, N);
+    uint32_t ties = 0;
+    if (keep > 0)
+        for (int i0 = lo; i0 < hi; i0 += 64) {
+            const int i = i0 + lane;
+            ties += __popcll(__ballot(i < hi && i < M && rank(i) == want));
+        }
+    __syncthreads();  // (sm_wave's last readers)
+    if (lane == 0) sm_wave[wave] = ties;
+    __syncthreads();
+    uint32_t before = 0;
+    for (int i = 0; i < wave; ++i) before += sm_wave[i];
+    for (int i0 = lo; i0 < hi; i0 += 64) {
+        const int i = i0 + lane;
+        const uint32_t r = keep > 0 && i < hi && i < M ? rank(i) : 0u;
+        const uint64_t tie = __ballot(keep > 0 && i < hi && i < M && r == want);
+        const bool stays = i < hi && (i >= M || (keep > 0 && (r > want || (r == want && before + __popcll(tie & ((1ull << lane) - 1)) < left))));
+        const uint64_t bits = __ballot(stays);
+        before += __popcll(tie);
+        if (lane == 0) sm_bits[i0 >> 5] = (uint32_t)bits;
+        if (lane == 32 && i0 + 32 < N) sm_bits[(i0 >> 5) + 1] = (uint32_t)(bits >> 32);
+    }
+    __syncthreads();
+    // (all ranks are read: mass may move now)
+    int done = 0;
+    for (int i0 = 0; i0 < N; i0 += MOVE) {
+        const int words = min(MOVE, N - i0 + 31) / 32;
+        if (wave == 0) {
+            const uint32_t c = lane < words ? __popc(sm_bits[(i0 >> 5) + lane]) : 0u;
+            uint32_t up = c;
+#pragma unroll
+            for (int off = 1; off < 64; off <<= 1) {
+                const uint32_t x = __shfl_up(up, off);
+                if (lane >= off) up += x;
+            }
+            if (lane <= MOVE / 32) sm_word[lane] = up - c;
+        }
+        __syncthreads();
+        const int count = sm_word[MOVE / 32];
+        for (int i = tid; i < MOVE; i += NT) {
+            if (i0 + i >= N) break;
+            const uint32_t w = sm_bits[(i0 + i) >> 5];
+            if (!(w >> (i & 31) & 1)) continue;
+            const int j = sm_word[i >> 5] + __popc(w & ((1u << (i & 31)) - 1));
+            list[j] = done + j == i0 + i ? make_uint2(NONE, NONE)
+                                         : make_uint2(row_of(a.c, s, h, i0 + i, bad), row_of(a.c, s, h, done + j, bad));
+        }
+        __syncthreads();
+        move_rows<HD>(a.c, layer, list, count);
+        done += count;
+        __syncthreads();
+    }
+    report(a.c, bad);
+}
+
+__global__ __launch_bounds__(256) void k_paged_evict_lens(PagedMoveArgs a)
+{
+    const int s = blockIdx.x * 256 + threadIdx.x;
+    if (s >= a.c.n_seqs) return;
+    const int N = a.c.lens[s];
+    if (N <= (int64_t)a.c.width * a.c.page && N > a.budget) a.new_lens[s] = a.budget;
+}
+
+// ---------------------------------------------------------------------------
+// launches
+
+template <bool BF, int HD> void append(const PagedAppendArgs &a, hipStream_t s)
+{
+    constexpr int HEADS = 256 / (HD / 8);
+    k_paged_append<BF, HD><<<dim3(a.n_rows, (a.Hq + 2 * a.c.H + HEADS - 1) / HEADS), 256, 0, s>>>(a);
+}
+
+template <int HD, bool BF, int RT> void attention(const PagedAttnArgs &a, const PagedCut &cut, hipStream_t s)
+{
+    const unsigned units = (unsigned)a.c.n_seqs * a.c.H;
+    if (cut.whole) {
+        k_paged_attn<HD, BF, RT, true><<<dim3(units, cut.blocks), 64 * NW, 0, s>>>(a);
+    } else {
+        k_paged_attn<HD, BF, RT, false><<<cut.groups, 64 * NW, 0, s>>>(a);
+        constexpr int AT_ONCE = 256 / (HD / 4);
+        k_paged_merge<HD, BF, RT><<<dim3(units, (cut.blocks * 16 * RT + AT_ONCE - 1) / AT_ONCE), 256, 0, s>>>(a);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_paged_append(const PagedAppendArgs &a, bool bf, hipStream_t s)
+{
+    if (a.c.hd == 64)
+        bf ? append<true, 64>(a, s) : append<false, 64>(a, s);
+    else
+        bf ? append<true, 128>(a, s) : append<false, 128>(a, s);
+    return hipGetLastError();
+}
+
+hipError_t launch_paged_attention(const PagedAttnArgs &a, bool bf, const PagedCut &cut, hipStream_t s)
+{
+    auto of = [&](auto hd_, auto bf_) {
+        constexpr int HD = decltype(hd_)::value;
+        constexpr bool BF = decltype(bf_)::value;
+        cut.rt == 1 ? attention<HD, BF, 1>(a, cut, s) : attention<HD, BF, 2>(a, cut, s);
+    };
+    using I64 = std::integral_constant<int, 64>;
+    using I128 = std::integral_constant<int, 128>;
+    if (a.c.hd == 64)
+        bf ? of(I64{}, std::true_type{}) : of(I64{}, std::false_type{});
+    else
+        bf ? of(I128{}, std::true_type{}) : of(I128{}, std::false_type{});
+    return hipGetLastError();
+}
+
+hipError_t launch_paged_mass(const PagedMassArgs &a, bool bf, hipStream_t s)
+{
+    if (a.c.hd == 64)
+        bf ? k_paged_mass<64, true><<<a.groups, 64 * NW, 0, s>>>(a) : k_paged_mass<64, false><<<a.groups, 64 * NW, 0, s>>>(a);
+    else
+        bf ? k_paged_mass<128, true><<<a.groups, 64 * NW, 0, s>>>(a) : k_paged_mass<128, false><<<a.groups, 64 * NW, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_paged_commit(const PagedMoveArgs &a, hipStream_t s)
+{
+    if (a.path) {
+        const unsigned units = (unsigned)a.c.L * a.c.n_seqs * a.c.H;
+        a.c.hd == 64 ? k_paged_commit<64><<<units, 512, 0, s>>>(a) : k_paged_commit<128><<<units, 512, 0, s>>>(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess || a.new_lens != a.c.lens) return e;
+    }
+    k_paged_commit_lens<<<(a.c.n_seqs + 255) / 256, 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_paged_evict(const PagedMoveArgs &a, hipStream_t s)
+{
+    const unsigned units = (unsigned)a.c.L * a.c.n_seqs * a.c.H;
+    const size_t bits = ((size_t)a.c.width * a.c.page + 31) / 32 * 4;
+    a.c.hd == 64 ? k_paged_evict<64><<<units, 512, bits, s>>>(a) : k_paged_evict<128><<<units, 512, bits, s>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.new_lens != a.c.lens) return e;
+    k_paged_evict_lens<<<(a.c.n_seqs + 255) / 256, 256, 0, s>>>(a);
+    return hipGetLastError();
+}

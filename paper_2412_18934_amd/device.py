@@ -150,3 +150,32 @@ class DeviceKVQ:
 
     def nbytes(self) -> int:
         return sum(t.nbytes for t in (self.k, self.v, self.scale, self.k_tail, self.v_tail))
+
+
+class DevicePaged:
+    """Paged KV cache (dv_paged): a pool of pages, the sequences' table (-1: no page) and their
+    committed slots.  n_heads counts KV heads; without mass nothing can be evicted."""
+
+    def __init__(self, n_layers, n_heads, head_dim, n_pages, page, n_seqs, table_stride, mass=True, device="cuda:0"):
+        self.k = torch.zeros((n_layers, n_pages, n_heads, page, head_dim), dtype=torch.bfloat16, device=device)
+        self.v = torch.zeros((n_layers, n_pages, n_heads, page // 32, head_dim, 32), dtype=torch.bfloat16, device=device)
+        self.mass = torch.zeros((n_layers, n_pages, n_heads, page), dtype=torch.float32, device=device) if mass else None
+        self.table = torch.full((n_seqs, table_stride), -1, dtype=torch.int32, device=device)
+        self.lens = torch.zeros(n_seqs, dtype=torch.int32, device=device)
+        self.fault = torch.zeros(1, dtype=torch.int32, device=device)
+        self.c = dv.dv_paged(self.k.data_ptr(), self.v.data_ptr(), self.mass.data_ptr() if mass else 0, self.table.data_ptr(),
+                             self.lens.data_ptr(), self.fault.data_ptr(), n_layers, n_heads, head_dim, n_pages, page, n_seqs,
+                             table_stride)
+
+    def rows(self, q, start=None, mask=None, scale=0.0, cap=0.0, max_rows=1, max_len=None) -> dv.dv_paged_rows:
+        """New rows with queries q [n_rows][n_heads][head_dim] (fp32 or bf16; heads and dims without gaps);
+        start, mask: device tensors or None.  The struct keeps the tensors."""
+        r = dv.dv_paged_rows(q.data_ptr(), q.stride(0), start.data_ptr() if start is not None else 0,
+                             mask.data_ptr() if mask is not None else 0, scale, cap,
+                             dv.DV_F32 if q.dtype == torch.float32 else dv.DV_BF16, q.shape[1], q.shape[0], max_rows,
+                             self.c.table_stride * self.c.page if max_len is None else max_len)
+        r.tensors = q, start, mask
+        return r
+
+    def nbytes(self) -> int:
+        return sum(t.nbytes for t in (self.k, self.v, self.mass, self.table, self.lens) if t is not None)

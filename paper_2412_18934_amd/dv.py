@@ -19,6 +19,7 @@ DV_F32, DV_BF16, DV_I8, DV_F8 = 0, 1, 2, 3
 DV_MAX_TREE = 64
 DV_NOALLOC_MAX_VOCAB = 262144
 DV_KVQ_TAIL = 96
+DV_ROPE_PLAIN, DV_ROPE_LINEAR, DV_ROPE_TURNS, DV_ROPE_LOG_TURNS = 0, 1, 2, 3
 DV_K_GEMM, DV_K_ATTN, DV_K_NORM, DV_K_OTHER = 0, 1, 2, 3
 
 # every symbol include/dv.h declares
@@ -28,7 +29,9 @@ EXPORTS = ("dv_verify_init", "dv_verify_step", "dv_verify_step_sampled", "dv_acc
            "dv_kv_commit", "dv_prefill", "dv_verify_free", "dv_last_error", "dv_tree_prepare",
            "dv_profile_enable", "dv_profile_read",
            "dv_kvq_store", "dv_kvq_load", "dv_kvq_advance", "dv_kvq_attention", "dv_kvq_attention_workspace",
-           "dv_verify_step_kvq", "dv_verify_step_kvq_sampled", "dv_prefill_kvq", "dv_kvq_commit")
+           "dv_verify_step_kvq", "dv_verify_step_kvq_sampled", "dv_prefill_kvq", "dv_kvq_commit",
+           "dv_rope_init", "dv_paged_append", "dv_paged_attention", "dv_paged_attention_workspace", "dv_paged_mass",
+           "dv_paged_commit", "dv_paged_evict")
 
 
 class DvError(RuntimeError):
@@ -72,6 +75,27 @@ class dv_kvq(ctypes.Structure):
                 ("k_tail", ctypes.c_void_p), ("v_tail", ctypes.c_void_p), ("n_layers", ctypes.c_int32),
                 ("n_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("format", ctypes.c_int32),
                 ("capacity", ctypes.c_int32), ("len", ctypes.c_int32)]
+
+
+class dv_paged(ctypes.Structure):
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("mass", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("lens", ctypes.c_void_p), ("fault", ctypes.c_void_p), ("n_layers", ctypes.c_int32),
+                ("n_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("n_pages", ctypes.c_int32),
+                ("page", ctypes.c_int32), ("n_seqs", ctypes.c_int32), ("table_stride", ctypes.c_int32)]
+
+
+class dv_paged_rows(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("q_stride", ctypes.c_int64), ("start", ctypes.c_void_p),
+                ("mask", ctypes.c_void_p), ("scale", ctypes.c_float), ("cap", ctypes.c_float),
+                ("dtype", ctypes.c_int32), ("n_heads", ctypes.c_int32), ("n_rows", ctypes.c_int32),
+                ("max_rows", ctypes.c_int32), ("max_len", ctypes.c_int32)]
+
+
+class dv_rope(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_double), ("factor", ctypes.c_double), ("low", ctypes.c_double),
+                ("high", ctypes.c_double), ("magnitude", ctypes.c_double), ("original_ctx", ctypes.c_int32),
+                ("scaling", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("freq", ctypes.c_double * 64)]
 
 
 class dv_accept(ctypes.Structure):
@@ -156,6 +180,21 @@ def lib():
         L.dv_prefill_kvq.restype = ctypes.c_int
         L.dv_kvq_commit.argtypes = [vp, kvqp, accp]
         L.dv_kvq_commit.restype = ctypes.c_int
+        pgp, rowsp, ropep = ctypes.POINTER(dv_paged), ctypes.POINTER(dv_paged_rows), ctypes.POINTER(dv_rope)
+        L.dv_rope_init.argtypes = [ropep]
+        L.dv_rope_init.restype = ctypes.c_int
+        L.dv_paged_append.argtypes = [pgp, i32, rowsp, ropep, vp, vp, i64, vp, i64, vp]
+        L.dv_paged_append.restype = ctypes.c_int
+        L.dv_paged_attention.argtypes = [pgp, i32, rowsp, vp, i64, vp, vp, i64, vp]
+        L.dv_paged_attention.restype = ctypes.c_int
+        L.dv_paged_attention_workspace.argtypes = [pgp, rowsp]
+        L.dv_paged_attention_workspace.restype = i64
+        L.dv_paged_mass.argtypes = [pgp, i32, rowsp, vp, vp, vp]
+        L.dv_paged_mass.restype = ctypes.c_int
+        L.dv_paged_commit.argtypes = [pgp, vp, i64, vp, vp, vp]
+        L.dv_paged_commit.restype = ctypes.c_int
+        L.dv_paged_evict.argtypes = [pgp, i32, i32, vp, vp]
+        L.dv_paged_evict.restype = ctypes.c_int
         _lib = L
     return _lib
 
@@ -355,6 +394,50 @@ def dv_prefill_kvq(h, tokens, kvq: dv_kvq) -> int:
 
 def dv_kvq_commit(h, kvq: dv_kvq, accept: dv_accept):
     _check(lib().dv_kvq_commit(h, kvq, accept), h)
+
+
+def dv_rope_init(rope: dv_rope) -> dv_rope:
+    """Checks the fields and fills freq."""
+    _check(lib().dv_rope_init(rope), None)
+    return rope
+
+
+def dv_paged_append(pg: dv_paged, layer: int, rows: dv_paged_rows, rope, positions: int, k: int, k_stride: int, v: int,
+                    v_stride: int, stream: int = 0):
+    """rope: dv_rope, or None (nothing is turned); positions (0: the slots' numbers) / k / v: device
+    addresses, strides in elements."""
+    _check(lib().dv_paged_append(pg, layer, rows, rope, positions or None, k or None, k_stride, v or None, v_stride,
+                                 stream or None), None)
+
+
+def dv_paged_attention_workspace(pg: dv_paged, rows: dv_paged_rows) -> int:
+    """Bytes of workspace that dv_paged_attention needs for such rows."""
+    size = int(lib().dv_paged_attention_workspace(pg, rows))
+    if size < 0:
+        _check(size, None)
+    return size
+
+
+def dv_paged_attention(pg: dv_paged, layer: int, rows: dv_paged_rows, out: int, out_stride: int, stats: int = 0,
+                       workspace: int = 0, workspace_bytes: int = 0, stream: int = 0):
+    """out / stats / workspace: device addresses, the stride in elements."""
+    _check(lib().dv_paged_attention(pg, layer, rows, out or None, out_stride, stats or None, workspace or None,
+                                    workspace_bytes, stream or None), None)
+
+
+def dv_paged_mass(pg: dv_paged, layer: int, rows: dv_paged_rows, stats: int, count: int = 0, stream: int = 0):
+    """stats / count (0: all rows): device addresses."""
+    _check(lib().dv_paged_mass(pg, layer, rows, stats or None, count or None, stream or None), None)
+
+
+def dv_paged_commit(pg: dv_paged, path: int, path_stride: int, path_len: int, new_lens: int, stream: int = 0):
+    """path (0: rows stay where they are) / path_len / new_lens: device addresses."""
+    _check(lib().dv_paged_commit(pg, path or None, path_stride, path_len or None, new_lens or None, stream or None), None)
+
+
+def dv_paged_evict(pg: dv_paged, budget: int, recent: int, new_lens: int, stream: int = 0):
+    """new_lens: device address."""
+    _check(lib().dv_paged_evict(pg, budget, recent, new_lens or None, stream or None), None)
 
 
 def dv_verify_free(h):
