@@ -135,7 +135,9 @@ int cut_of(const dv_paged *c, const dv_paged_rows *r, PagedCut *cut)
     int n_cu = 0;
     const hipError_t e = current_cus(&n_cu);
     if (e != hipSuccess) return set_err(nullptr, DV_EHIP, "compute units: %s", hipGetErrorString(e));
-    *cut = paged_cut(c->n_seqs, c->n_heads, r->n_heads / c->n_heads, r->max_rows, r->max_len, n_cu);
+    *cut = paged_cut(c->n_seqs, c->n_heads, r->n_heads / c->n_heads, r->n_rows, r->max_rows, r->max_len, n_cu);
+    if (cut->grid > MAX_GROUPS || (int64_t)c->n_seqs * c->n_heads * cut->blocks > MAX_GROUPS)
+        return set_err(nullptr, DV_EINVAL, "%d rows of %d heads are too many for one call", r->n_rows, r->n_heads);
     return DV_OK;
 }
 
@@ -245,7 +247,7 @@ int dv_paged_attention(const dv_paged *c, int32_t layer, const dv_paged_rows *r,
     a.stats = reinterpret_cast<float2 *>(stats);
     a.groups = cut.groups;
     a.part_o = static_cast<float *>(workspace);
-    if (need) a.part_ml = reinterpret_cast<float2 *>(a.part_o + (size_t)2 * cut.groups * 16 * cut.rt * c->head_dim);
+    if (need) a.part_ml = reinterpret_cast<float2 *>(a.part_o + (size_t)cut.groups * 16 * cut.rt * c->head_dim);
     return launched(launch_paged_attention(a, r->dtype == DV_BF16, cut, static_cast<hipStream_t>(stream)), "paged attention");
 }
 

@@ -5,6 +5,7 @@
 // 2^32: row r is K's elements r hd .. + hd, V's column r % 32 of the 32-slot tile
 // r / 32 (hd x 32, dim-major), and mass's element r.  A 32-slot tile of keys and its tile of
 // values start at the same element.
+#include <algorithm>
 #include <type_traits>
 
 #include "dv_device.h"
@@ -22,36 +23,109 @@ __device__ __forceinline__ void report(const PagedView &c, bool bad)
     if (bad && c.fault) *c.fault = 1;  // (every writer writes the same)
 }
 
-// NT threads sum up all sequences' tiles, a run of sequences each.
-template <int NT> struct Line {
-    int64_t total, mine, sum;  // all tiles; those before this thread's sequences; theirs
-    int s0, s1;
-    template <typename W> __device__ __forceinline__ Line(int n_seqs, W w)
+// Consecutive tiles of a unit
+struct Segment {
+    Seq q;
+    int s, h, b, t0, t1;
+    bool whole;  // all of the unit's tiles
+};
+
+// Sums over the lanes below `n` (a power of two or more than they are; the others hold 0): all, and up
+// to each.  A step is two trips through LDS, so there are no more than n needs.
+__device__ __forceinline__ int64_t wave_sum(int64_t x, int n)
+{
+    for (int off = 1; off < 64 && off < n; off <<= 1) x += __shfl_xor((long long)x, off);
+    return (int64_t)__builtin_amdgcn_readfirstlane((uint32_t)(x >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)x);
+}
+__device__ __forceinline__ int64_t wave_prefix(int64_t x, int n)
+{
+    for (int off = 1; off < 64 && off < n; off <<= 1) {
+        const int64_t y = __shfl_up((long long)x, off);
+        if ((int)(threadIdx.x & 63) >= off) x += y;
+    }
+    return x;
+}
+
+// All pieces of a call in one line: sequences in order, of each its units, of each its pieces.
+// The waves of a workgroup go through the sequences side by side, 64 at a time, a lane each, so up to
+// that many are read once.
+struct Pieces {
+    const PagedView &c;
+    const PagedRowsView &r;
+    const int block;
+    int size;       // tiles of a piece, about
+    int base;       // the lanes' first sequence
+    int64_t before, all;  // pieces before the lanes' sequences, and with them
+    Seq mine;       // the lane's sequence, its load and the pieces of its units
+    Load load;
+    int cut;
+
+    __device__ __forceinline__ void read(int first, bool &bad)
     {
-        __shared__ int64_t sm_sum[NT / 64];
-        const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-        const int per = (n_seqs + NT - 1) / NT;
-        s0 = min(tid * per, n_seqs);
-        s1 = min(s0 + per, n_seqs);
-        sum = 0;
-        for (int s = s0; s < s1; ++s) sum += w(s);
-        int64_t up = sum;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const int64_t x = __shfl_up((long long)up, off);
-            if (lane >= off) up += x;
+        const int i = first + (threadIdx.x & 63);
+        base = first;
+        mine = {0, 0, 0};
+        if (i < c.n_seqs) mine = seq_of(c, r.start, r.n_rows, i, PAGED_MAX_NEW, bad);
+        load = load_of(c, mine, r.G, block);
+    }
+    __device__ __forceinline__ void count()
+    {
+        cut = load.units ? pieces_of(load.tiles, size) : 0;
+        all = before + wave_sum((int64_t)load.units * cut, c.n_seqs - base);
+    }
+    __device__ __forceinline__ Pieces(const PagedView &c_, const PagedRowsView &r_, int block_, int most, int least, bool &bad)
+        : c(c_), r(r_), block(block_), before(0)
+    {
+        int64_t units = 0, tiles = 0;
+        for (int first = 0; first < c.n_seqs; first += 64) {
+            read(first, bad);
+            units += load.units;
+            tiles += (int64_t)load.units * load.tiles;
         }
-        if (lane == 63) sm_sum[wave] = up;
-        __syncthreads();
-        mine = up - sum;
-        total = 0;
-#pragma unroll
-        for (int i = 0; i < NT / 64; ++i) {
-            if (i < wave) mine += sm_sum[i];
-            total += sm_sum[i];
+        size = piece_size(wave_sum(units, c.n_seqs), wave_sum(tiles, c.n_seqs), most, least);
+        if (c.n_seqs > 64) read(0, bad);
+        count();
+    }
+    // the lanes come to the 64 sequences among which `reached` holds; false if there are none
+    template <typename F> __device__ __forceinline__ bool seek(F reached, bool &bad)
+    {
+        while (!reached()) {
+            if (base + 64 >= c.n_seqs) return false;
+            before = all;
+            read(base + 64, bad);
+            count();
         }
+        return true;
+    }
+    // piece number `at`, which is not below those of earlier calls; false if there are not so many
+    __device__ __forceinline__ bool take(int64_t at, Segment &x, bool &bad)
+    {
+        if (!seek([&] { return at < all; }, bad)) return false;
+        const int64_t sum = (int64_t)load.units * cut, up = before + wave_prefix(sum, c.n_seqs - base);
+        const int lane = __builtin_ctzll(__ballot(at < up));
+        const int units = __builtin_amdgcn_readlane(load.units, lane), tiles = __builtin_amdgcn_readlane(load.tiles, lane);
+        const int n = __builtin_amdgcn_readlane(cut, lane), i = (int)(at - __shfl((long long)(up - sum), lane));
+        const int unit = (uint32_t)i / (uint32_t)n, p = i - unit * n, blocks = (uint32_t)units / (uint32_t)c.H;
+        x.q = {__builtin_amdgcn_readlane(mine.first, lane), __builtin_amdgcn_readlane(mine.n, lane),
+               __builtin_amdgcn_readlane(mine.len, lane)};
+        x.s = base + lane;
+        x.h = __builtin_amdgcn_readfirstlane((uint32_t)unit / (uint32_t)blocks);
+        x.b = __builtin_amdgcn_readfirstlane(unit - x.h * blocks);
+        x.t0 = __builtin_amdgcn_readfirstlane(piece_start(tiles, n, p));
+        x.t1 = __builtin_amdgcn_readfirstlane(piece_start(tiles, n, p + 1));
+        x.whole = n == 1;
+        return true;
     }
 };
+
+// Piece number `at`, false if there is none.  (A workgroup has one: in a loop over pieces the compiler
+// keeps 42 registers more.)
+__device__ __forceinline__ bool piece_at(const PagedView &c, const PagedRowsView &r, int block, int most, int least, int64_t at,
+                                         Segment &x, bool &bad)
+{
+    Pieces p(c, r, block, most, least, bad);
+    return p.take(at, x, bad);
+}
 
 // ---------------------------------------------------------------------------
 // conversions
@@ -241,7 +315,7 @@ template <bool BF, int HD> __global__ __launch_bounds__(256) void k_paged_append
 }
 
 // ---------------------------------------------------------------------------
-// Attention of new rows over pages, split over the slots and joined.
+// Attention of new rows over pages, split over the slots and combined.
 //
 //   z_ij = scale (q_i . k_j), capped: cap tanh(z / cap); over the slots that row i sees
 //   o_i = sum_j exp(z_ij - m_i) v_j / sum_j exp(z_ij - m_i), m_i the largest z: one pass,
@@ -252,8 +326,21 @@ template <bool BF, int HD> __global__ __launch_bounds__(256) void k_paged_append
 //   are keys 8 (i / 4) + 4 t + i % 4, so D gives lane (n, g) the scores of row n for the keys
 //   8 g .. + 8, which are the B operand of O^T = V^T P^T; its D has 4 consecutive dims of
 //   row n.  A row's numbers belong to lanes n + 16 g, only its maximum crosses lanes.
-
-constexpr int NW = 8;  // waves of a workgroup
+//
+// Roundings: fp32 queries and weights enter as three bf16 parts (all 24 bits); with bf16 rows the query is one
+// part and a weight two (16 bits: the output keeps 8).  Scores, maxima and sums are fp32.
+//
+// A wave has a tile of its own, so no barrier stands between tiles; K's registers take the next
+// tile when the last row tile's scores are made, V's after the products: up to 128 KB per CU in flight.
+// What bounds it: the pages' bytes.  532 MB of one sequence at 5.75 TB/s (92.6 us with the combining launch of
+// 7), 48 ragged ones (438 MB) at 4.9 TB/s; short calls 2.5 us until a workgroup knows its piece, 3 to 6
+// until its first tile is there, 2 for the waves' sums.
+// Measured and taken: 4 waves twice per CU for 8 once (93 for 101 us, 48 ragged sequences); V's loads past
+// the caches where a tile is read once (92 for 102, one sequence; K's too: its lines are read in halves, 36 to
+// 41 us for eight 16-node trees); queries from LDS and not from 48 registers.
+// Not taken: equal shares of all tiles that run over units' ends (the eight trees 39 to 50 for 31 us: each end
+// costs a workgroup 4 us); 12 waves per CU (spills with fp32 rows, no gain with bf16); pieces in a loop per workgroup
+// (42 registers more).
 
 // A 32-slot tile in registers, 16 bytes per lane and load
 template <int HD> struct Tile {
@@ -268,11 +355,14 @@ template <int HD> struct Tile {
             for (int c = 0; c < HD / 32; ++c)
                 k[t * (HD / 32) + c] = *reinterpret_cast<const u32x4 *>(p + 4 * t * HD + 32 * c);
     }
-    __device__ __forceinline__ void load_v(const uint16_t *base, uint32_t row, int lane)
+    template <bool ONCE> __device__ __forceinline__ void load_v(const uint16_t *base, uint32_t row, int lane)
     {
         const uint16_t *p = base + (size_t)row * HD + (lane & 15) * PAGED_TILE + 8 * (lane >> 4);
 #pragma unroll
-        for (int dt = 0; dt < HD / 16; ++dt) v[dt] = *reinterpret_cast<const u32x4 *>(p + dt * 16 * PAGED_TILE);
+        for (int dt = 0; dt < HD / 16; ++dt) {
+            const u32x4 *at = reinterpret_cast<const u32x4 *>(p + dt * 16 * PAGED_TILE);
+            v[dt] = ONCE ? __builtin_nontemporal_load(at) : *at;
+        }
     }
 };
 
@@ -284,7 +374,7 @@ __device__ __forceinline__ uint32_t tile_rows(const PagedView &c, int s, int h, 
 }
 
 // Queries of a row block as B operands in LDS, NP parts: [rt][dims / 32][part][lane]
-template <int HD, bool BF, int RT>
+template <int HD, bool BF, int RT, int NW>
 __device__ __forceinline__ void stage_queries(const PagedRowsView &r, const Seq &q, int h, int row0, u32x4 *to)
 {
     constexpr int NP = BF ? 1 : 3, NC = HD / 32;
@@ -395,26 +485,29 @@ __device__ __forceinline__ void finish(const PagedAttnArgs &a, const Seq &q, int
     if (d0 == 0 && a.stats) a.stats[token * ((int64_t)a.c.H * a.r.G) + head] = make_float2(m, l);
 }
 
-template <int HD, bool BF, int RT, bool WHOLE> __global__ __launch_bounds__(64 * NW) void k_paged_attn(PagedAttnArgs a)
+template <int HD, bool BF, int RT, int NW, bool WHOLE> __global__ __launch_bounds__(64 * NW, 2) void k_paged_attn(PagedAttnArgs a)
 {
     constexpr int NC = HD / 32, ND = HD / 16, NP = BF ? 1 : 3, NV = BF ? 2 : 3;
     constexpr int SUMS = NW * 16 * RT * (HD + 4) * 4, PARTS = RT * NC * NP * 1024;
-    __shared__ __align__(16) char sm[SUMS > PARTS ? SUMS : PARTS];  // queries, later the waves' sums
+    __shared__ __align__(16) char sm[SUMS > PARTS ? SUMS : PARTS];  // queries, then the waves' sums
     __shared__ float sm_m[NW][16 * RT], sm_l[NW][16 * RT];
-    __shared__ int64_t sm_before;
-    __shared__ int sm_s;
     u32x4 *qs = reinterpret_cast<u32x4 *>(sm);
     float(*sm_o)[16 * RT][HD + 4] = reinterpret_cast<float(*)[16 * RT][HD + 4]>(sm);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     bool bad = false;
 
-    // tiles [t0, t1) of row block b; slot: where partial sums go, below 0: these are all tiles
-    auto segment = [&](const Seq &q, int s, int h, int b, int t0, int t1, int slot) {
-        const int row0 = b * 16 * RT, rows = q.n * a.r.G;
+    // piece: where partial sums go
+    auto segment = [&](const Segment &x, int piece) {
+        const Seq q = x.q;
+        const int row0 = x.b * 16 * RT, rows = q.n * a.r.G, t1 = x.t1;
         const int plain = q.len / PAGED_TILE;  // tiles below: all slots committed
-        uint32_t ids = tile_rows(a.c, s, h, t0 + wave, NW, t1, lane, bad);
-        __syncthreads();
-        stage_queries<HD, BF, RT>(a.r, q, h, row0, qs);
+        uint32_t ids = tile_rows(a.c, x.s, x.h, x.t0 + wave, NW, t1, lane, bad);
+        Tile<HD> kv;
+        uint32_t row = __builtin_amdgcn_readlane(ids, 0);
+        // (loads never branch: where there is no tile they read the pool's first)
+        kv.load_k(a.c.k, row == NONE ? 0 : row, lane);
+        kv.template load_v<RT == 1>(a.c.v, row == NONE ? 0 : row, lane);
+        stage_queries<HD, BF, RT, NW>(a.r, q, x.h, row0, qs);
         uint64_t mask[RT];
         float m_run[RT], l_run[RT];  // (l_run: of the lane's own keys)
         f32x4 o[RT][ND];
@@ -426,27 +519,16 @@ template <int HD, bool BF, int RT, bool WHOLE> __global__ __launch_bounds__(64 *
 #pragma unroll
             for (int dt = 0; dt < ND; ++dt) o[rt][dt] = (f32x4){0.f, 0.f, 0.f, 0.f};
         }
-        Tile<HD> x;
-        int at = 0;
-        uint32_t row = __builtin_amdgcn_readlane(ids, 0);
-        // (loads never branch: where there is no tile they read the pool's first)
-        x.load_k(a.c.k, row == NONE ? 0 : row, lane);
-        x.load_v(a.c.v, row == NONE ? 0 : row, lane);
         __syncthreads();
-        for (int t = t0 + wave; t < t1; t += NW) {
+        int at = 0;
+        for (int t = x.t0 + wave; t < t1; t += NW) {
+            if (!BF || RT > 1) asm volatile("" ::: "memory");  // (queries stay in LDS: in registers they take too many)
             if (++at == 64) {
-                ids = tile_rows(a.c, s, h, t + NW, NW, t1, lane, bad);
+                ids = tile_rows(a.c, x.s, x.h, t + NW, NW, t1, lane, bad);
                 at = 0;
             }
             const uint32_t next = __builtin_amdgcn_readlane(ids, at), from = next == NONE ? 0 : next;
             const bool part = t >= plain;
-            float w[RT][8];
-            each<RT>([&](auto rt_) {
-                constexpr int rt = decltype(rt_)::value;
-                if (RT > 1 && row0 + 16 * rt >= rows) return;
-                scores8<HD, BF>(x.k, qs + rt * NC * NP * 64, lane, w[rt]);
-            });
-            x.load_k(a.c.k, from, lane);
             bool odd = false;
             uint32_t see[RT];
             if (part) {
@@ -460,80 +542,82 @@ template <int HD, bool BF, int RT, bool WHOLE> __global__ __launch_bounds__(64 *
                 for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        x.v[dt][i] &= (2 * i < mine ? 0xffffu : 0u) | (2 * i + 1 < mine ? 0xffff0000u : 0u);
-                        any |= (x.v[dt][i] & 0x7f80u) == 0x7f80u || (x.v[dt][i] & 0x7f800000u) == 0x7f800000u;
+                        kv.v[dt][i] &= (2 * i < mine ? 0xffffu : 0u) | (2 * i + 1 < mine ? 0xffff0000u : 0u);
+                        any |= (kv.v[dt][i] & 0x7f80u) == 0x7f80u || (kv.v[dt][i] & 0x7f800000u) == 0x7f800000u;
                     }
                 odd = __any(any);
                 if (odd)
 #pragma unroll
-                    for (int dt = 0; dt < ND; ++dt) x.v[dt] = finite(x.v[dt]);
+                    for (int dt = 0; dt < ND; ++dt) kv.v[dt] = finite(kv.v[dt]);
             }
-            if (row != NONE)
-                each<RT>([&](auto rt_) {
-                    constexpr int rt = decltype(rt_)::value;
-                    if (RT > 1 && row0 + 16 * rt >= rows) return;
-                    float(&s8)[8] = w[rt];
-                    scaled(a.r, s8);
-                    if (part)
+            each<RT>([&](auto rt_) {
+                constexpr int rt = decltype(rt_)::value;
+                const bool none = row == NONE || (RT > 1 && row0 + 16 * rt >= rows);
+                float s8[8];
+                if (!none) scores8<HD, BF>(kv.k, qs + rt * NC * NP * 64, lane, s8);
+                if (rt == RT - 1) kv.load_k(a.c.k, from, lane);
+                if (none) return;
+                scaled(a.r, s8);
+                if (part)
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) s8[i] = see[rt] >> i & 1 ? s8[i] : -INFINITY;
-                    float mt = s8[0];
+                    for (int i = 0; i < 8; ++i) s8[i] = see[rt] >> i & 1 ? s8[i] : -INFINITY;
+                float mt = s8[0];
 #pragma unroll
-                    for (int i = 1; i < 8; ++i) mt = fmaxf(mt, s8[i]);
-                    if (__any(mt > m_run[rt])) {
-                        mt = fmaxf(mt, __shfl_xor(mt, 16));
-                        mt = fmaxf(mt, __shfl_xor(mt, 32));
-                        const float mnew = fmaxf(m_run[rt], mt);
-                        const float alpha = m_run[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_run[rt] - mnew) * LOG2E);
-                        l_run[rt] *= alpha;
+                for (int i = 1; i < 8; ++i) mt = fmaxf(mt, s8[i]);
+                if (__any(mt > m_run[rt])) {
+                    mt = fmaxf(mt, __shfl_xor(mt, 16));
+                    mt = fmaxf(mt, __shfl_xor(mt, 32));
+                    const float mnew = fmaxf(m_run[rt], mt);
+                    const float alpha = m_run[rt] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m_run[rt] - mnew) * LOG2E);
+                    l_run[rt] *= alpha;
 #pragma unroll
-                        for (int dt = 0; dt < ND; ++dt)
+                    for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) o[rt][dt][j] *= alpha;
-                        m_run[rt] = mnew;
-                    }
-                    float ps = 0.f;
+                        for (int j = 0; j < 4; ++j) o[rt][dt][j] *= alpha;
+                    m_run[rt] = mnew;
+                }
+                float ps = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
-                        s8[i] = s8[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((s8[i] - m_run[rt]) * LOG2E);
-                        ps += s8[i];
-                    }
-                    l_run[rt] += ps;
-                    u32x4 p[NV];
-                    if constexpr (BF)
-                        split2(s8, p);
-                    else
-                        split3(s8, p);
+                for (int i = 0; i < 8; ++i) {
+                    s8[i] = s8[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((s8[i] - m_run[rt]) * LOG2E);
+                    ps += s8[i];
+                }
+                l_run[rt] += ps;
+                u32x4 p[NV];
+                if constexpr (BF)
+                    split2(s8, p);
+                else
+                    split3(s8, p);
 #pragma unroll
-                    for (int i = 0; i < NV; ++i)
+                for (int i = 0; i < NV; ++i)
 #pragma unroll
-                        for (int dt = 0; dt < ND; ++dt) o[rt][dt] = mfma_bf16(x.v[dt], p[i], o[rt][dt]);
-                    if (!odd) return;
-                    // an infinity or NaN counts for the rows that see its key, however small its weight
-                    const uint16_t *vt = a.c.v + (size_t)row * HD;
-                    const int left = min(PAGED_TILE, q.len + q.n - t * PAGED_TILE);
+                    for (int dt = 0; dt < ND; ++dt) o[rt][dt] = mfma_bf16(kv.v[dt], p[i], o[rt][dt]);
+                if (!odd) return;
+                // an infinity or NaN counts for the rows that see its key, however small its weight
+                const uint16_t *vt = a.c.v + (size_t)row * HD;
+                const int left = min(PAGED_TILE, q.len + q.n - t * PAGED_TILE);
 #pragma unroll 1
-                    for (int key = 0; key < left; ++key) {
-                        float pk = s8[0];
+                for (int key = 0; key < left; ++key) {
+                    float pk = s8[0];
 #pragma unroll
-                        for (int i = 1; i < 8; ++i) pk = (key & 7) == i ? s8[i] : pk;
-                        pk = __shfl(pk, 16 * (key >> 3) + n);
-                        const bool seen = __shfl((int)see[rt], 16 * (key >> 3) + n) >> (key & 7) & 1;
+                    for (int i = 1; i < 8; ++i) pk = (key & 7) == i ? s8[i] : pk;
+                    pk = __shfl(pk, 16 * (key >> 3) + n);
+                    const bool seen = __shfl((int)see[rt], 16 * (key >> 3) + n) >> (key & 7) & 1;
 #pragma unroll
-                        for (int dt = 0; dt < ND; ++dt)
+                    for (int dt = 0; dt < ND; ++dt)
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const float y = bf2f(vt[(dt * 16 + 4 * g + j) * PAGED_TILE + key]);
-                                if (!__builtin_isfinite(y) && seen) o[rt][dt][j] += pk * y;
-                            }
-                    }
-                });
-            x.load_v(a.c.v, from, lane);
+                        for (int j = 0; j < 4; ++j) {
+                            const float y = bf2f(vt[(dt * 16 + 4 * g + j) * PAGED_TILE + key]);
+                            if (!__builtin_isfinite(y) && seen) o[rt][dt][j] += pk * y;
+                        }
+                }
+            });
+            kv.template load_v<RT == 1>(a.c.v, from, lane);
             row = next;
         }
 
         // combine the waves, in their order
-        const int rows_here = min(16 * RT, rows - row0), active = min(NW, t1 - t0);
+        const int rows_here = min(16 * RT, rows - row0), active = min(NW, t1 - x.t0);
         __syncthreads();
         if (wave < active)
             each<RT>([&](auto rt_) {
@@ -556,112 +640,116 @@ template <int HD, bool BF, int RT, bool WHOLE> __global__ __launch_bounds__(64 *
             float m = -INFINITY, l = 0.f, ov[4] = {0.f, 0.f, 0.f, 0.f};
             for (int w = 0; w < active; ++w) m = fmaxf(m, sm_m[w][i]);
             for (int w = 0; w < active; ++w) {
-                const float mw = sm_m[w][i], f = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((mw - m) * LOG2E);
                 // (a wave whose every score is NaN has a largest of -infinity and a sum of NaN)
-                l += mw == -INFINITY ? sm_l[w][i] : f * sm_l[w][i];
+                const float mw = sm_m[w][i], f = mw == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((mw - m) * LOG2E);
+                l = fmaf(f, sm_l[w][i], l);
                 const f32x4 o4 = *reinterpret_cast<const f32x4 *>(&sm_o[w][i][d0]);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) ov[j] = mw == -INFINITY ? ov[j] + o4[j] : fmaf(f, o4[j], ov[j]);
+                for (int j = 0; j < 4; ++j) ov[j] = fmaf(f, o4[j], ov[j]);
             }
-            if (slot < 0) {
-                finish<HD, BF>(a, q, h, row0 + i, d0, m, l, ov);
+            if (x.whole) {
+                finish<HD, BF>(a, q, x.h, row0 + i, d0, m, l, ov);
             } else {
-                const int64_t p = (int64_t)slot * 16 * RT + i;
+                const int64_t p = (int64_t)piece * 16 * RT + i;
                 *reinterpret_cast<float4 *>(a.part_o + p * HD + d0) = make_float4(ov[0], ov[1], ov[2], ov[3]);
                 if (d0 == 0) a.part_ml[p] = make_float2(m, l);
             }
         }
     };
 
+    Segment x{};
     if constexpr (WHOLE) {
-        const int s = blockIdx.x / a.c.H, h = blockIdx.x % a.c.H;
-        const Seq q = seq_of(a.c, a.r.start, a.r.n_rows, s, PAGED_MAX_NEW, bad);
-        const Load w = load_of(a.c, q, a.r.G, 16 * RT);
-        for (int b = blockIdx.y; b < w.units / a.c.H; b += gridDim.y) segment(q, s, h, b, 0, w.tiles, -1);
-    } else {
-        const int me = blockIdx.x;
-        auto weight = [&](int s) {
-            const Load w = load_of(a.c, seq_of(a.c, a.r.start, a.r.n_rows, s, PAGED_MAX_NEW, bad), a.r.G, 16 * RT);
-            return (int64_t)w.units * w.tiles;
-        };
-        const Line<64 * NW> line(a.c.n_seqs, weight);
-        const int groups = shares_of(line.total, a.groups);
-        int64_t at = me < groups ? share_start(line.total, me, groups) : 0;
-        const int64_t end = me < groups ? share_start(line.total, me + 1, groups) : 0;
-        if (at < end) {  // (the same in all threads)
-            if (at >= line.mine && at < line.mine + line.sum) {
-                int64_t before = line.mine;
-                for (int s = line.s0; s < line.s1; ++s) {
-                    const int64_t w = weight(s);
-                    if (at < before + w) {
-                        sm_s = s;
-                        sm_before = before;
-                        break;
-                    }
-                    before += w;
-                }
-            }
+        x.s = blockIdx.x / a.c.H;
+        x.h = blockIdx.x % a.c.H;
+        x.q = seq_of(a.c, a.r.start, a.r.n_rows, x.s, PAGED_MAX_NEW, bad);
+        const Load w = load_of(a.c, x.q, a.r.G, 16 * RT);
+        x.t1 = w.tiles;
+        x.whole = true;
+        for (x.b = blockIdx.y; x.b < w.units / a.c.H; x.b += gridDim.y) {
+            segment(x, 0);
             __syncthreads();
-            int64_t before = sm_before;
-            for (int s = sm_s; at < end && s < a.c.n_seqs; ++s) {
-                const Seq q = seq_of(a.c, a.r.start, a.r.n_rows, s, PAGED_MAX_NEW, bad);
-                const Load w = load_of(a.c, q, a.r.G, 16 * RT);
-                const int64_t all = (int64_t)w.units * w.tiles;
-                while (at < end && at < before + all) {
-                    const int unit = (int)((at - before) / w.tiles), t0 = (int)((at - before) % w.tiles);
-                    const int t1 = (int)min((int64_t)w.tiles, t0 + (end - at)), blocks = w.units / a.c.H;
-                    segment(q, s, unit / blocks, unit % blocks, t0, t1,
-                            t0 == 0 && t1 == w.tiles ? -1 : 2 * me + (t0 == 0));
-                    at += t1 - t0;
-                }
-                before += all;
-            }
         }
+    } else {
+        if (piece_at(a.c, a.r, 16 * RT, a.groups, NW, blockIdx.x, x, bad)) segment(x, blockIdx.x);
     }
     report(a.c, bad);
 }
 
-// The shares of a row block combined, in their order, in a launch of its own.  Workgroup
-// (sequence and KV head, rows): HD / 4 threads have 4 dims of a row each.
-template <int HD, bool BF, int RT> __global__ __launch_bounds__(256) void k_paged_merge(PagedAttnArgs a)
+// The pieces of a row block combined in a launch of its own.  Workgroup (sequence and KV head, rows):
+// HD / 4 threads have 4 dims of a row each, and LANES such groups every LANES-th piece; they are
+// combined in LDS.  The order is fixed, so are the results.
+template <int HD, bool BF, int RT, int NW, int LANES> __global__ __launch_bounds__(256) void k_paged_merge(PagedAttnArgs a)
 {
-    __shared__ int64_t sm_before;
-    constexpr int PER = HD / 4, AT_ONCE = 256 / PER;
+    constexpr int PER = HD / 4, AT_ONCE = 256 / PER / LANES, STEP = LANES == 1 ? 2 : 4;
+    __shared__ __align__(16) float sm_o[AT_ONCE][LANES][HD];
+    __shared__ float2 sm_ml[AT_ONCE][LANES];
     const int tid = threadIdx.x, s = blockIdx.x / a.c.H, h = blockIdx.x % a.c.H, d0 = 4 * (tid % PER);
+    const int part = tid / PER % LANES, mine = tid / PER / LANES;
     bool bad = false;
-    auto weight = [&](int i) {
-        const Load w = load_of(a.c, seq_of(a.c, a.r.start, a.r.n_rows, i, PAGED_MAX_NEW, bad), a.r.G, 16 * RT);
-        return (int64_t)w.units * w.tiles;
-    };
-    const Line<256> line(a.c.n_seqs, weight);
-    if (s >= line.s0 && s < line.s1) {
-        int64_t before = line.mine;
-        for (int i = line.s0; i < s; ++i) before += weight(i);
-        sm_before = before;
-    }
-    __syncthreads();
-    const Seq q = seq_of(a.c, a.r.start, a.r.n_rows, s, PAGED_MAX_NEW, bad);
-    const Load w = load_of(a.c, q, a.r.G, 16 * RT);
-    const int rows = q.n * a.r.G, blocks = w.units / a.c.H, groups = shares_of(line.total, a.groups);
-    for (int row = blockIdx.y * AT_ONCE + tid / PER; row < rows; row += gridDim.y * AT_ONCE) {
-        const int b = row / (16 * RT), i = row % (16 * RT);
-        const int64_t first = sm_before + ((int64_t)h * blocks + b) * w.tiles, last = first + w.tiles - 1;
-        const int g0 = share_of(line.total, first, groups), g1 = share_of(line.total, last, groups);
-        if (g0 == g1) continue;  // (one workgroup had it all)
+    Pieces pieces(a.c, a.r, 16 * RT, a.groups, NW, bad);
+    pieces.seek([&] { return s < pieces.base + 64; }, bad);
+    const int from = s - pieces.base, n = __builtin_amdgcn_readlane(pieces.cut, from);
+    if (n < 2) return;  // (nothing, or one workgroup had it all)
+    const int64_t own = (int64_t)pieces.load.units * pieces.cut;
+    const int64_t before = __shfl((long long)(pieces.before + wave_prefix(own, a.c.n_seqs - pieces.base) - own), from);
+    const Seq q = {__builtin_amdgcn_readlane(pieces.mine.first, from), __builtin_amdgcn_readlane(pieces.mine.n, from),
+                   __builtin_amdgcn_readlane(pieces.mine.len, from)};
+    const int rows = q.n * a.r.G, blocks = (rows + 16 * RT - 1) / (16 * RT);
+    for (int row0 = blockIdx.y * AT_ONCE; row0 < rows; row0 += gridDim.y * AT_ONCE) {
+        const int row = row0 + mine, b = row / (16 * RT), i = row % (16 * RT);
+        const int64_t first = before + ((int64_t)h * blocks + b) * n;
         float m = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-        for (int g = g0; g <= g1; ++g) m = fmaxf(m, a.part_ml[(int64_t)(2 * g + (g == g0)) * 16 * RT + i].x);
-        for (int g = g0; g <= g1; ++g) {
-            const int64_t p = (int64_t)(2 * g + (g == g0)) * 16 * RT + i;
-            const float2 ml = a.part_ml[p];
-            const float f = ml.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((ml.x - m) * LOG2E);
-            const float4 x = *reinterpret_cast<const float4 *>(a.part_o + p * HD + d0);
-            l = fmaf(f, ml.y, l);
-            o[0] = fmaf(f, x.x, o[0]);
-            o[1] = fmaf(f, x.y, o[1]);
-            o[2] = fmaf(f, x.z, o[2]);
-            o[3] = fmaf(f, x.w, o[3]);
+        if (row < rows)
+            for (int g = part; g < n; g += LANES * STEP) {
+                float2 ml[STEP];
+                float4 x[STEP];
+#pragma unroll
+                for (int u = 0; u < STEP; ++u) {
+                    const int64_t p = (first + min(g + u * LANES, n - 1)) * 16 * RT + i;
+                    ml[u] = a.part_ml[p];
+                    x[u] = *reinterpret_cast<const float4 *>(a.part_o + p * HD + d0);
+                }
+                float top = m;
+#pragma unroll
+                for (int u = 0; u < STEP; ++u) top = g + u * LANES < n ? fmaxf(top, ml[u].x) : top;
+                const float f0 = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((m - top) * LOG2E);
+                l *= f0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) o[j] *= f0;
+#pragma unroll
+                for (int u = 0; u < STEP; ++u) {
+                    if (g + u * LANES >= n) break;
+                    const float f = ml[u].x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((ml[u].x - top) * LOG2E);
+                    l = fmaf(f, ml[u].y, l);
+                    o[0] = fmaf(f, x[u].x, o[0]);
+                    o[1] = fmaf(f, x[u].y, o[1]);
+                    o[2] = fmaf(f, x[u].z, o[2]);
+                    o[3] = fmaf(f, x[u].w, o[3]);
+                }
+                m = top;
+            }
+        __syncthreads();
+        *reinterpret_cast<float4 *>(&sm_o[mine][part][d0]) = make_float4(o[0], o[1], o[2], o[3]);
+        if (d0 == 0) sm_ml[mine][part] = make_float2(m, l);
+        __syncthreads();
+        if (part == 0 && row < rows) {
+            float top = -INFINITY, ov[4] = {0.f, 0.f, 0.f, 0.f};
+            l = 0.f;
+#pragma unroll
+            for (int k = 0; k < LANES; ++k) top = fmaxf(top, sm_ml[mine][k].x);
+#pragma unroll
+            for (int k = 0; k < LANES; ++k) {
+                const float2 ml = sm_ml[mine][k];
+                const float f = ml.x == -INFINITY ? 1.f : __builtin_amdgcn_exp2f((ml.x - top) * LOG2E);
+                const float4 x = *reinterpret_cast<const float4 *>(&sm_o[mine][k][d0]);
+                l = fmaf(f, ml.y, l);
+                ov[0] = fmaf(f, x.x, ov[0]);
+                ov[1] = fmaf(f, x.y, ov[1]);
+                ov[2] = fmaf(f, x.z, ov[2]);
+                ov[3] = fmaf(f, x.w, ov[3]);
+            }
+            finish<HD, BF>(a, q, h, row, d0, top, l, ov);
         }
-        finish<HD, BF>(a, q, h, row, d0, m, l, o);
     }
 }
 
@@ -670,12 +758,24 @@ template <int HD, bool BF, int RT> __global__ __launch_bounds__(256) void k_page
 // from K alone, half of what attention read; a tile belongs to one wave, which adds its
 // rows in order, so nothing is atomic.
 
-template <int HD, bool BF> __global__ __launch_bounds__(64 * NW) void k_paged_mass(PagedMassArgs a)
+// Sum over the 16 lanes of a row of lanes, in all of them: rotations inside the row
+__device__ __forceinline__ float row_sum(float x)
 {
-    constexpr int NC = HD / 32, NP = BF ? 1 : 3, RT = 4;  // row tiles at a time
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int y = i == 0   ? __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x128, 0xf, 0xf, false)
+                      : i == 1 ? __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x124, 0xf, 0xf, false)
+                      : i == 2 ? __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x122, 0xf, 0xf, false)
+                               : __builtin_amdgcn_update_dpp(0, __float_as_int(x), 0x121, 0xf, 0xf, false);
+        x += __int_as_float(y);
+    }
+    return x;
+}
+
+template <int HD, bool BF> __global__ __launch_bounds__(512) void k_paged_mass(PagedMassArgs a)
+{
+    constexpr int NC = HD / 32, NP = BF ? 1 : 3, RT = 4, NW = 8;  // row tiles at a time
     __shared__ __align__(16) u32x4 qs[RT * NC * NP * 64];
-    __shared__ int64_t sm_before;
-    __shared__ int sm_s;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     bool bad = false;
 
@@ -685,7 +785,7 @@ template <int HD, bool BF> __global__ __launch_bounds__(64 * NW) void k_paged_ma
         for (int row0 = 0; row0 < rows; row0 += 16 * RT) {
             uint32_t ids = tile_rows(a.c, s, h, t0 + wave, NW, t1, lane, bad);
             __syncthreads();
-            stage_queries<HD, BF, RT>(a.r, q, h, row0, qs);
+            stage_queries<HD, BF, RT, NW>(a.r, q, h, row0, qs);
             uint64_t mask[RT];
             float m[RT], f[RT];  // a row that does not count: f < 0
 #pragma unroll
@@ -703,14 +803,17 @@ template <int HD, bool BF> __global__ __launch_bounds__(64 * NW) void k_paged_ma
             Tile<HD> x;
             int at = 0;
             uint32_t row = __builtin_amdgcn_readlane(ids, 0);
+            // (lane (n, g): key 8 g + n % 8)
+            float had = a.c.mass[(size_t)(row == NONE ? 0 : row) + 8 * g + (n & 7)];
             x.load_k(a.c.k, row == NONE ? 0 : row, lane);
             __syncthreads();
             for (int t = t0 + wave; t < t1; t += NW) {
+                asm volatile("" ::: "memory");  // (queries stay in LDS: in registers they take too many)
                 if (++at == 64) {
                     ids = tile_rows(a.c, s, h, t + NW, NW, t1, lane, bad);
                     at = 0;
                 }
-                const uint32_t next = __builtin_amdgcn_readlane(ids, at);
+                const uint32_t next = __builtin_amdgcn_readlane(ids, at), from = next == NONE ? 0 : next;
                 float sum[8] = {};
                 each<RT>([&](auto rt_) {
                     constexpr int rt = decltype(rt_)::value;
@@ -726,58 +829,24 @@ template <int HD, bool BF> __global__ __launch_bounds__(64 * NW) void k_paged_ma
                         sum[i] += (see >> i & 1) && !(f[rt] < 0.f) ? w : 0.f;
                     }
                 });
-                x.load_k(a.c.k, next == NONE ? 0 : next, lane);
+                const float old = had;
+                had = a.c.mass[(size_t)from + 8 * g + (n & 7)];
+                x.load_k(a.c.k, from, lane);
+                float mine = 0.f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-#pragma unroll
-                    for (int off = 1; off < 16; off <<= 1) sum[i] += __shfl_xor(sum[i], off);
-                if (row != NONE && n == 0) {
-                    float *to = a.c.mass + (size_t)row + 8 * g;
-                    const int mine = min(max(q.len + q.n - (t * PAGED_TILE + 8 * g), 0), 8);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if (i < mine) to[i] += sum[i];
+                for (int i = 0; i < 8; ++i) {
+                    const float all = row_sum(sum[i]);
+                    mine = (n & 7) == i ? all : mine;
                 }
+                if (row != NONE && n < 8 && t * PAGED_TILE + 8 * g + n < q.len + q.n)
+                    a.c.mass[(size_t)row + 8 * g + n] = old + mine;
                 row = next;
             }
         }
     };
 
-    auto weight = [&](int s) {
-        const Load w = load_of(a.c, seq_of(a.c, a.r.start, a.r.n_rows, s, PAGED_MAX_NEW, bad), a.r.G, 1 << 30);
-        return (int64_t)w.units * w.tiles;
-    };
-    const Line<64 * NW> line(a.c.n_seqs, weight);
-    int64_t at = share_start(line.total, blockIdx.x, gridDim.x);
-    const int64_t end = share_start(line.total, blockIdx.x + 1, gridDim.x);
-    if (at < end) {
-        if (at >= line.mine && at < line.mine + line.sum) {
-            int64_t before = line.mine;
-            for (int s = line.s0; s < line.s1; ++s) {
-                const int64_t w = weight(s);
-                if (at < before + w) {
-                    sm_s = s;
-                    sm_before = before;
-                    break;
-                }
-                before += w;
-            }
-        }
-        __syncthreads();
-        int64_t before = sm_before;
-        for (int s = sm_s; at < end && s < a.c.n_seqs; ++s) {
-            const Seq q = seq_of(a.c, a.r.start, a.r.n_rows, s, PAGED_MAX_NEW, bad);
-            const Load w = load_of(a.c, q, a.r.G, 1 << 30);
-            const int64_t all = (int64_t)w.units * w.tiles;
-            while (at < end && at < before + all) {
-                const int h = (int)((at - before) / w.tiles), t0 = (int)((at - before) % w.tiles);
-                const int t1 = (int)min((int64_t)w.tiles, t0 + (end - at));
-                segment(q, s, h, t0, t1);
-                at += t1 - t0;
-            }
-            before += all;
-        }
-    }
+    Segment x;
+    if (piece_at(a.c, a.r, 1 << 30, gridDim.x, NW, blockIdx.x, x, bad)) segment(x.q, x.s, x.h, x.t0, x.t1);
     report(a.c, bad);
 }
 
@@ -1019,15 +1088,24 @@ template <bool BF, int HD> void append(const PagedAppendArgs &a, hipStream_t s)
     k_paged_append<BF, HD><<<dim3(a.n_rows, (a.Hq + 2 * a.c.H + HEADS - 1) / HEADS), 256, 0, s>>>(a);
 }
 
-template <int HD, bool BF, int RT> void attention(const PagedAttnArgs &a, const PagedCut &cut, hipStream_t s)
+template <int HD, bool BF, int RT, int NW> void attention(const PagedAttnArgs &a, const PagedCut &cut, hipStream_t s)
 {
     const unsigned units = (unsigned)a.c.n_seqs * a.c.H;
     if (cut.whole) {
-        k_paged_attn<HD, BF, RT, true><<<dim3(units, cut.blocks), 64 * NW, 0, s>>>(a);
+        k_paged_attn<HD, BF, RT, NW, true><<<dim3(units, cut.blocks), 64 * NW, 0, s>>>(a);
     } else {
-        k_paged_attn<HD, BF, RT, false><<<cut.groups, 64 * NW, 0, s>>>(a);
-        constexpr int AT_ONCE = 256 / (HD / 4);
-        k_paged_merge<HD, BF, RT><<<dim3(units, (cut.blocks * 16 * RT + AT_ONCE - 1) / AT_ONCE), 256, 0, s>>>(a);
+        k_paged_attn<HD, BF, RT, NW, false><<<(unsigned)cut.grid, 64 * NW, 0, s>>>(a);
+        // (rows beyond the grid's are looped over)
+        auto merge = [&](auto lanes_) {
+            constexpr int LANES = decltype(lanes_)::value, AT_ONCE = 256 / (HD / 4) / LANES;
+            const int groups = std::min((cut.blocks * 16 * RT + AT_ONCE - 1) / AT_ONCE, 4096);
+            k_paged_merge<HD, BF, RT, NW, LANES><<<dim3(units, groups), 256, 0, s>>>(a);
+        };
+        // pieces of a unit, about: with many, 8 groups of threads share them
+        if (cut.groups > 4 * (int64_t)units * cut.blocks)
+            merge(std::integral_constant<int, 8>{});
+        else
+            merge(std::integral_constant<int, 1>{});
     }
 }
 
@@ -1047,7 +1125,7 @@ hipError_t launch_paged_attention(const PagedAttnArgs &a, bool bf, const PagedCu
     auto of = [&](auto hd_, auto bf_) {
         constexpr int HD = decltype(hd_)::value;
         constexpr bool BF = decltype(bf_)::value;
-        cut.rt == 1 ? attention<HD, BF, 1>(a, cut, s) : attention<HD, BF, 2>(a, cut, s);
+        cut.rt == 1 ? attention<HD, BF, 1, 4>(a, cut, s) : attention<HD, BF, 2, 4>(a, cut, s);
     };
     using I64 = std::integral_constant<int, 64>;
     using I128 = std::integral_constant<int, 128>;
@@ -1061,9 +1139,9 @@ hipError_t launch_paged_attention(const PagedAttnArgs &a, bool bf, const PagedCu
 hipError_t launch_paged_mass(const PagedMassArgs &a, bool bf, hipStream_t s)
 {
     if (a.c.hd == 64)
-        bf ? k_paged_mass<64, true><<<a.groups, 64 * NW, 0, s>>>(a) : k_paged_mass<64, false><<<a.groups, 64 * NW, 0, s>>>(a);
+        bf ? k_paged_mass<64, true><<<a.groups, 512, 0, s>>>(a) : k_paged_mass<64, false><<<a.groups, 512, 0, s>>>(a);
     else
-        bf ? k_paged_mass<128, true><<<a.groups, 64 * NW, 0, s>>>(a) : k_paged_mass<128, false><<<a.groups, 64 * NW, 0, s>>>(a);
+        bf ? k_paged_mass<128, true><<<a.groups, 512, 0, s>>>(a) : k_paged_mass<128, false><<<a.groups, 512, 0, s>>>(a);
     return hipGetLastError();
 }
 

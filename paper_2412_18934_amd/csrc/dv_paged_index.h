@@ -51,8 +51,8 @@ PAGED_FN uint32_t row_of(const PagedView &c, int s, int h, int slot, bool &bad)
     return (id * (uint32_t)c.H + (uint32_t)h) * (uint32_t)c.page + ((uint32_t)slot - p * (uint32_t)c.page);
 }
 
-// The work of a call is its 32-slot tiles in one line: sequences in order, of each its
-// units (KV heads times row blocks of `block` rows) in order, of each the tiles.
+// The work of a call on a sequence: units (KV heads times row blocks of `block` rows), each of
+// them 32-slot tiles.
 struct Load {
     int units, tiles;
 };
@@ -62,23 +62,22 @@ PAGED_FN Load load_of(const PagedView &c, const Seq &q, int G, int block)
     return {c.H * (int)(((int64_t)q.n * G + block - 1) / block), (q.len + q.n + PAGED_TILE - 1) / PAGED_TILE};
 }
 
-// Shares of a line: no more than tiles, so that none is empty (a joined unit's shares all have a part).
-PAGED_FN int shares_of(int64_t total, int groups) { return total < groups ? (int)total : groups; }
+// a / b for numbers that are hardly ever over 32 bits (a 64-bit division is some 100 instructions)
+PAGED_FN int64_t quotient(int64_t a, int64_t b)
+{
+    return (a | b) >> 32 ? a / b : (int64_t)((uint32_t)a / (uint32_t)b);
+}
 
-// Workgroup g of `groups` has the tiles [share_start(g), share_start(g + 1)): total g / groups,
-// rounded down, without a product that leaves 64 bits.
-PAGED_FN int64_t share_start(int64_t total, int g, int groups)
+// Units are cut into pieces of about `size` tiles, equal ones of a unit, so that all are `most`
+// pieces at most: a unit has less than tiles / size + 1.  With `most` units or more none is cut.
+PAGED_FN int piece_size(int64_t units, int64_t tiles, int most, int least)
 {
-    return total / groups * g + total % groups * g / groups;
+    if (units >= most) return 1 << 30;
+    const int64_t size = quotient(tiles + most - units - 1, most - units);
+    return size < least ? least : (int)size;
 }
-PAGED_FN int share_of(int64_t total, int64_t tile, int groups)
-{
-    int g = (int)((double)tile / (double)total * groups);
-    g = g < groups ? g : groups - 1;
-    while (share_start(total, g + 1, groups) <= tile) ++g;
-    while (share_start(total, g, groups) > tile) --g;
-    return g;
-}
+PAGED_FN int pieces_of(int tiles, int size) { return (int)(((uint32_t)tiles + (uint32_t)size - 1) / (uint32_t)size); }
+PAGED_FN int piece_start(int tiles, int pieces, int i) { return (int)((uint64_t)tiles * i / pieces); }
 
 // Whether entry i of sequence s's path of n can be, and whether its length can
 PAGED_FN bool path_ok(const PagedMoveArgs &a, int s, int i, int n)

@@ -191,9 +191,9 @@ uint32_t t_row(int width, int page, int n_pages, int H, const int32_t *table, in
     *bad = b;
     return r;
 }
-int t_shares(int64_t total, int groups) { return shares_of(total, groups); }
-int64_t t_share(int64_t total, int g, int groups) { return share_start(total, g, groups); }
-int t_owner(int64_t total, int64_t tile, int groups) { return share_of(total, tile, groups); }
+int t_size(int64_t units, int64_t tiles, int most, int least) { return piece_size(units, tiles, most, least); }
+int t_pieces(int tiles, int size) { return pieces_of(tiles, size); }
+int t_start(int tiles, int pieces, int i) { return piece_start(tiles, pieces, i); }
 int t_commit(int width, int page, int len, const int32_t *path, int64_t stride, int n, const int32_t *at)
 {
     const int32_t lens[1] = {len}, ns[1] = {n};
@@ -205,11 +205,11 @@ int t_commit(int width, int page, int len, const int32_t *path, int64_t stride, 
     return 1;
 }
 uint32_t t_rank(float m) { return rank_of(m); }
-void t_cut(int seqs, int heads, int group, int rows, int len, int cu, int64_t *out)
+void t_cut(int seqs, int heads, int group, int n_rows, int rows, int len, int cu, int64_t *out)
 {
-    const PagedCut c = paged_cut(seqs, heads, group, rows, len, cu);
+    const PagedCut c = paged_cut(seqs, heads, group, n_rows, rows, len, cu);
     out[0] = c.rt, out[1] = c.blocks, out[2] = c.groups, out[3] = c.whole, out[4] = (int64_t)paged_attention_bytes(c, 128);
-    out[5] = paged_mass_groups(seqs, heads, len, cu);
+    out[5] = c.grid, out[6] = paged_mass_groups(seqs, heads, len, cu);
 }
 }
 """
@@ -226,9 +226,7 @@ def lib(tmp_path_factory):
                     "-o", out], check=True)
     L = ctypes.CDLL(out)
     i64 = ctypes.c_int64
-    L.t_share.argtypes, L.t_share.restype = [i64, ctypes.c_int, ctypes.c_int], i64
-    L.t_shares.argtypes = [i64, ctypes.c_int]
-    L.t_owner.argtypes = [i64, i64, ctypes.c_int]
+    L.t_size.argtypes = [i64, i64, ctypes.c_int, ctypes.c_int]
     L.t_row.restype = L.t_rank.restype = ctypes.c_uint32
     L.t_rank.argtypes = [ctypes.c_float]
     L.t_commit.argtypes = [ctypes.c_int] * 3 + [ctypes.c_void_p, i64, ctypes.c_int, ctypes.c_void_p]
@@ -271,19 +269,25 @@ def test_pages_outside_the_pool_are_no_rows(lib):
     assert r == 4095 * 2 ** 20 - 1
 
 
-@pytest.mark.parametrize("total", [1, 2, 7, 255, 256, 257, 1000, 99991, 2 ** 40 + 12345, 2 ** 59 + 1])
-@pytest.mark.parametrize("groups", [1, 3, 8, 256, 512])
-def test_shares_cover_everything_once(lib, total, groups):
-    groups = lib.t_shares(total, groups)
-    assert lib.t_shares(0, groups) == 0
-    at = [lib.t_share(total, g, groups) for g in range(groups + 1)]
-    assert at[0] == 0 and at[-1] == total and all(a < b for a, b in zip(at, at[1:]))
-    assert max(b - a for a, b in zip(at, at[1:])) - min(b - a for a, b in zip(at, at[1:])) <= 1
-    rng = np.random.default_rng(total % 1000)
-    tiles = {0, total - 1} | {int(x) for x in rng.integers(0, total, 60)} | {x for a in at for x in (a - 1, a) if 0 <= x < total}
-    for t in tiles:
-        g = lib.t_owner(total, t, groups)
-        assert at[g] <= t < at[g + 1]
+@pytest.mark.parametrize("most", [1, 5, 256, 1000, 1 << 20])
+def test_pieces_fit_and_cover_their_unit(lib, most):
+    """No more pieces than room for their sums, whatever the lengths; each unit's are whole, even and not empty."""
+    rng = np.random.default_rng(most)
+    for trial in range(200):
+        seqs = int(rng.integers(1, 40))
+        units = rng.integers(0, 50, seqs) * (rng.random(seqs) < 0.9)
+        tiles = np.maximum(1, (2.0 ** rng.uniform(0, rng.choice([3, 10, 25]), seqs)).astype(np.int64))
+        size = lib.t_size(int(units.sum()), int((units * tiles).sum()), most, 4)
+        n = [lib.t_pieces(int(t), size) for t in tiles]
+        total = sum(int(u) * p for u, p in zip(units, n))
+        assert total <= max(most, int(units.sum()))
+        if units.sum() >= most:
+            assert set(n) == {1}
+        for t, p in zip(tiles.tolist(), n):
+            at = [lib.t_start(t, p, i) for i in {0, 1, p // 2, p - 1, p} if i <= p]
+            assert lib.t_start(t, p, 0) == 0 and lib.t_start(t, p, p) == t and 1 <= p <= t and len(at)
+            for i in (0, p // 2, p - 1):
+                assert 0 < lib.t_start(t, p, i + 1) - lib.t_start(t, p, i) <= max(size, 1)
 
 
 @pytest.mark.parametrize("length,path,n,ok", [
@@ -309,16 +313,20 @@ def test_ranks_order_masses(lib):
 
 
 @pytest.mark.parametrize("cu", [256, 64])
-def test_every_row_block_and_share_has_work(lib, cu):
-    out = (ctypes.c_int64 * 6)()
-    for seqs in (1, 3, 48, 65536):
+def test_every_row_block_has_a_workgroup(lib, cu):
+    """Also where the sequences have more rows than max_rows says."""
+    out, rng = (ctypes.c_int64 * 7)(), np.random.default_rng(0)
+    for seqs in (1, 3, 48, 6000):
         for heads in (1, 8, 40):
             for group in (1, 4, 1024):
                 for n in (1, 16, 64):
-                    for length in (0, 1, 500, 768, 4100, 1 << 30):
-                        lib.t_cut(seqs, heads, group, n, length, cu, out)
-                        rt, blocks, groups, whole, size, mass = out
+                    for length in (0, 1, 500, 1500, 4100, 1 << 30):
+                        rows = rng.integers(0, 65, seqs)
+                        rows[0] = max(rows[0], 1)
+                        lib.t_cut(seqs, heads, group, int(rows.sum()), n, length, cu, out)
+                        rt, blocks, groups, whole, size, grid, mass = out
                         assert 16 * rt * blocks >= n * group > 16 * rt * (blocks - 1)
                         assert whole == (groups == 0) == (size == 0)
-                        assert whole or 1 <= groups <= cu and size == 2 * groups * 16 * rt * 130 * 4
-                        assert 1 <= mass <= 2 * cu
+                        units = heads * int((-(-rows * group // (16 * rt))).sum())
+                        assert grid >= max(units, groups) and mass >= seqs * heads
+                        assert whole or groups >= 2 * cu and size == groups * 16 * rt * 130 * 4
