@@ -10,6 +10,7 @@
 #define PAGED_TILE 32        // slots of a V tile, and of a step of attention
 #define PAGED_MAX_NEW 64     // new rows of a sequence that a mask names
 #define PAGED_MAX_PIECES (1 << 20)
+#define PAGED_MAX_RANKS 10240   // slots of a sequence whose ranks an eviction keeps in LDS
 #define PAGED_MAX_EVICT 262144  // slots of a sequence that an eviction marks in LDS, a bit each
 
 // The cache; layer-wise calls have k, v and mass at their layer.

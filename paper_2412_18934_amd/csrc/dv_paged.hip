@@ -851,12 +851,10 @@ template <int HD, bool BF> __global__ __launch_bounds__(512) void k_paged_mass(P
 }
 
 // ---------------------------------------------------------------------------
-// Commit and eviction move rows of a (layer, sequence, KV head) to lower slots, in order.
-// Source slots increase, and each is at least its destination; so a wave that always
-// has the same columns of K (or dims of V) can go through the list by itself: what it
-// overwrites is no later row's source, and a step's loads stand before its stores.
-
-constexpr int MOVE = 1024;  // rows of a list
+// Commit moves rows of a (layer, sequence, KV head) to lower slots, in order.  Source slots increase, and
+// each is at least its destination; so a wave that always has the same columns of K (or dims of V) can
+// go through the list by itself: what it overwrites is no later row's source, and a step's loads stand before
+// its stores.
 
 // Rows list[i].x to list[i].y, i < count; NONE in either: not moved.  8 waves.
 template <int HD> __device__ __forceinline__ void move_rows(const PagedView &c, int layer, const uint2 *list, int count)
@@ -864,7 +862,7 @@ template <int HD> __device__ __forceinline__ void move_rows(const PagedView &c, 
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const size_t base = (size_t)layer * c.n_pages * c.H * c.page;
     if (wave < 4) {  // K: a quarter of the columns
-        constexpr int CH = HD / 32, ROWS = 64 / CH, U = 4;  // 16 bytes each
+        constexpr int CH = HD / 32, ROWS = 64 / CH, U = 8;  // 16 bytes each
         uint16_t *k = c.k + base * HD + (wave * CH + lane % CH) * 8;
         for (int i0 = 0; i0 < count; i0 += ROWS * U) {
             u32x4 x[U];
@@ -889,22 +887,28 @@ template <int HD> __device__ __forceinline__ void move_rows(const PagedView &c, 
                 mass[e.y] = m;
             }
         }
-    } else {  // V: a quarter of the dims, 32 rows at a time, two dims a load
-        constexpr int U = HD / 8;
+    } else {  // V: a quarter of the dims, two of them and 32 rows a load
+        constexpr int U = HD / 8, T = 2;
         uint16_t *v = c.v + base * HD + ((wave - 4) * (HD / 4) + lane / 32) * PAGED_TILE;
-        for (int i0 = 0; i0 < count; i0 += 32) {
-            const int i = i0 + lane % 32;
-            uint2 e = i < count ? list[i] : make_uint2(NONE, NONE);
-            const bool moves = e.x != NONE && e.y != NONE;
-            uint16_t x[U];
-            const uint16_t *from = v + (size_t)(e.x / PAGED_TILE) * HD * PAGED_TILE + e.x % PAGED_TILE;
-            uint16_t *to = v + (size_t)(e.y / PAGED_TILE) * HD * PAGED_TILE + e.y % PAGED_TILE;
-            if (moves) {
+        for (int i0 = 0; i0 < count; i0 += 32 * T) {
+            uint16_t x[T][U], *to[T];
+            bool moves[T];
 #pragma unroll
-                for (int u = 0; u < U; ++u) x[u] = from[2 * u * PAGED_TILE];
+            for (int t = 0; t < T; ++t) {
+                const int i = i0 + 32 * t + lane % 32;
+                const uint2 e = i < count ? list[i] : make_uint2(NONE, NONE);
+                moves[t] = e.x != NONE && e.y != NONE;
+                to[t] = v + (size_t)(e.y / PAGED_TILE) * HD * PAGED_TILE + e.y % PAGED_TILE;
+                const uint16_t *from = v + (size_t)(e.x / PAGED_TILE) * HD * PAGED_TILE + e.x % PAGED_TILE;
+                if (moves[t])
 #pragma unroll
-                for (int u = 0; u < U; ++u) to[2 * u * PAGED_TILE] = x[u];
+                    for (int u = 0; u < U; ++u) x[t][u] = from[2 * u * PAGED_TILE];
             }
+#pragma unroll
+            for (int t = 0; t < T; ++t)
+                if (moves[t])
+#pragma unroll
+                    for (int u = 0; u < U; ++u) to[t][2 * u * PAGED_TILE] = x[t][u];
         }
     }
 }
@@ -946,19 +950,28 @@ __global__ __launch_bounds__(256) void k_paged_commit_lens(PagedMoveArgs a)
 }
 
 // ---------------------------------------------------------------------------
-// Eviction, a workgroup for each (layer, sequence, KV head): the mass that separates what stays
-// is found digit by digit from the top, counted in LDS; then every slot's bit is made (equal
-// masses: the lower slots), and the slots whose bit is set move up.
+// Eviction, a workgroup for each (layer, sequence, KV head).  The mass that separates what stays is found digit by
+// digit from the top, counted in LDS; then every slot's bit is made (equal masses: the lower
+// slots), and the slots whose bit is set move up, 24 tiles of source slots at a time: K's rows as they are;
+// of V, whose slots are its fastest dimension, 32 dims of all 24 tiles are laid into LDS and
+// gathered there, 8 slots of a dim to a store.  Source slots increase and each is at least its
+// destination: what a step overwrites is in registers or LDS by then, and no later step's source.
 
-template <int HD> __global__ __launch_bounds__(512) void k_paged_evict(PagedMoveArgs a)
+constexpr int MOVE_TILES = 24, MOVE = MOVE_TILES * PAGED_TILE, DIMS = 32, V_DIM = 72;  // V_DIM: bytes of a dim's tile in LDS
+
+template <int HD, bool RANKS> __global__ __launch_bounds__(512, 4) void k_paged_evict(PagedMoveArgs a)
 {
-    constexpr int NT = 512, BITS = 11, BINS = 1 << BITS;
+    constexpr int NT = 512, BITS = 11, BINS = 1 << BITS, BUF = MOVE_TILES * DIMS * V_DIM;
+    static_assert(PAGED_MAX_RANKS * 4 + BINS * 4 <= BUF, "ranks and counts stand where V's tiles come");
     extern __shared__ uint32_t sm_bits[];
-    __shared__ uint32_t hist[BINS];
+    __shared__ __align__(16) char sm[BUF];
     __shared__ uint2 list[MOVE];
-    __shared__ uint32_t sm_wave[NT / 64], sm_bin, sm_above, sm_word[MOVE / 32 + 1];
+    __shared__ __align__(16) uint16_t off[MOVE + 16];  // of the rows' numbers in sm, from the 8 slots that hold the first row on
+    __shared__ uint32_t sm_wave[NT / 64], sm_bin, sm_above, sm_word[MOVE_TILES + 1], from_tile[MOVE_TILES], to_tile[MOVE_TILES + 2];
+    __shared__ int sm_first;
+    uint32_t *hist = reinterpret_cast<uint32_t *>(sm), *ranks = hist + BINS;
     const int h = blockIdx.x % a.c.H, s = blockIdx.x / a.c.H % a.c.n_seqs, layer = blockIdx.x / a.c.H / a.c.n_seqs;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, N = a.c.lens[s];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), N = a.c.lens[s];
     const bool first = h == 0 && layer == 0 && tid == 0, apart = a.new_lens != a.c.lens;
     if (N < 0 || N > (int64_t)a.c.width * a.c.page || N <= a.budget) {
         if (first) report(a.c, N < 0 || N > (int64_t)a.c.width * a.c.page);
@@ -968,11 +981,27 @@ template <int HD> __global__ __launch_bounds__(512) void k_paged_evict(PagedMove
     if (first && apart) a.new_lens[s] = a.budget;
     bool bad = false;
     const int M = N - a.recent, keep = a.budget - a.recent;  // keep < M
-    const float *mass = a.c.mass + (size_t)layer * a.c.n_pages * a.c.H * a.c.page;
-    auto rank = [&](int slot) {
+    const size_t base = (size_t)layer * a.c.n_pages * a.c.H * a.c.page;
+    float *mass = a.c.mass + base;
+    auto look = [&](int slot) {
         const uint32_t r = row_of(a.c, s, h, slot, bad);
         return r == NONE ? 0u : rank_of(mass[r]);
     };
+    if (RANKS && keep > 0) {
+        constexpr int U = 4;
+        for (int i0 = tid; i0 < M; i0 += U * NT) {
+            uint32_t r[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) r[u] = i0 + u * NT < M ? row_of(a.c, s, h, i0 + u * NT, bad) : NONE;
+            float m[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) m[u] = mass[r[u] == NONE ? 0 : r[u]];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (i0 + u * NT < M) ranks[i0 + u * NT] = r[u] == NONE ? 0u : rank_of(m[u]);
+        }
+    }
+    auto rank = [&](int slot) { return RANKS ? ranks[slot] : look(slot); };
 
     // the keep-th largest rank, and how many of that rank stay
     uint32_t want = 0, left = keep;
@@ -994,9 +1023,9 @@ template <int HD> __global__ __launch_bounds__(512) void k_paged_evict(PagedMove
             for (int i = 0; i < 4; ++i) sum += c[i] = hist[BINS - 1 - 4 * tid - i];
             uint32_t up = sum;
 #pragma unroll
-            for (int off = 1; off < 64; off <<= 1) {
-                const uint32_t x = __shfl_up(up, off);
-                if (lane >= off) up += x;
+            for (int o = 1; o < 64; o <<= 1) {
+                const uint32_t x = __shfl_up(up, o);
+                if (lane >= o) up += x;
             }
             if (lane == 63) sm_wave[wave] = up;
             __syncthreads();
@@ -1025,9 +1054,11 @@ template <int HD> __global__ __launch_bounds__(512) void k_paged_evict(PagedMove
         }
     __syncthreads();  // (sm_wave's last readers)
     if (lane == 0) sm_wave[wave] = ties;
+    if (tid == 0) sm_first = N;
     __syncthreads();
     uint32_t before = 0;
     for (int i = 0; i < wave; ++i) before += sm_wave[i];
+    int mine = N;  // the wave's first slot that goes
     for (int i0 = lo; i0 < hi; i0 += 64) {
         const int i = i0 + lane;
         const uint32_t r = keep > 0 && i < hi && i < M ? rank(i) : 0u;
@@ -1035,38 +1066,127 @@ template <int HD> __global__ __launch_bounds__(512) void k_paged_evict(PagedMove
         const bool stays = i < hi && (i >= M || (keep > 0 && (r > want || (r == want && before + __popcll(tie & ((1ull << lane) - 1)) < left))));
         const uint64_t bits = __ballot(stays);
         before += __popcll(tie);
+        if (~bits && mine == N) mine = i0 + __builtin_ctzll(~bits);
         if (lane == 0) sm_bits[i0 >> 5] = (uint32_t)bits;
         if (lane == 32 && i0 + 32 < N) sm_bits[(i0 >> 5) + 1] = (uint32_t)(bits >> 32);
     }
+    if (lane == 0) atomicMin(&sm_first, mine);
     __syncthreads();
     // (all ranks are read: mass may move now)
-    int done = 0;
-    for (int i0 = 0; i0 < N; i0 += MOVE) {
-        const int words = min(MOVE, N - i0 + 31) / 32;
+
+    constexpr int PASSES = HD / DIMS, ROWS = MOVE / PASSES, U = 6;
+    static_assert(MOVE_TILES * DIMS * 4 == U * NT && ROWS * (HD / 8) == U * NT, "16 bytes a thread, U times");
+    uint16_t *k = a.c.k + base * HD, *v = a.c.v + base * HD;
+    const int words = (N + 31) / 32;
+    int done = sm_first / 32 * 32;  // (slots before it stay where they are)
+    for (int w0 = done / 32; w0 < words; w0 += MOVE_TILES) {
         if (wave == 0) {
-            const uint32_t c = lane < words ? __popc(sm_bits[(i0 >> 5) + lane]) : 0u;
+            const uint32_t c = lane < MOVE_TILES && w0 + lane < words ? __popc(sm_bits[w0 + lane]) : 0u;
             uint32_t up = c;
 #pragma unroll
-            for (int off = 1; off < 64; off <<= 1) {
-                const uint32_t x = __shfl_up(up, off);
-                if (lane >= off) up += x;
+            for (int o = 1; o < 64; o <<= 1) {
+                const uint32_t x = __shfl_up(up, o);
+                if (lane >= o) up += x;
             }
-            if (lane <= MOVE / 32) sm_word[lane] = up - c;
+            if (lane <= MOVE_TILES) sm_word[lane] = up - c;
+            if (lane < MOVE_TILES) from_tile[lane] = c ? row_of(a.c, s, h, (w0 + lane) * 32, bad) : NONE;
+        } else if (wave == 1 && lane < MOVE_TILES + 2) {
+            const int to = (done / 32 + lane) * 32;
+            to_tile[lane] = to < a.budget ? row_of(a.c, s, h, to, bad) : NONE;
         }
+        for (int i = tid; i < MOVE + 16; i += NT) off[i] = 0xffff;
         __syncthreads();
-        const int count = sm_word[MOVE / 32];
+        const int count = sm_word[MOVE_TILES];
         for (int i = tid; i < MOVE; i += NT) {
-            if (i0 + i >= N) break;
-            const uint32_t w = sm_bits[(i0 + i) >> 5];
+            if (w0 + (i >> 5) >= words) break;
+            const uint32_t w = sm_bits[w0 + (i >> 5)];
             if (!(w >> (i & 31) & 1)) continue;
-            const int j = sm_word[i >> 5] + __popc(w & ((1u << (i & 31)) - 1));
-            list[j] = done + j == i0 + i ? make_uint2(NONE, NONE)
-                                         : make_uint2(row_of(a.c, s, h, i0 + i, bad), row_of(a.c, s, h, done + j, bad));
+            const int j = sm_word[i >> 5] + __popc(w & ((1u << (i & 31)) - 1)), to = done + j;
+            const uint32_t x = from_tile[i >> 5], y = to_tile[(to >> 5) - (done >> 5)];
+            const bool moves = x != NONE && y != NONE && to != w0 * 32 + i;
+            list[j] = moves ? make_uint2(x + (i & 31), y + (to & 31)) : make_uint2(NONE, NONE);
+            if (x != NONE && y != NONE) off[(done & 7) + j] = (uint16_t)((i >> 5) * DIMS * V_DIM + (i & 31) * 2);
         }
         __syncthreads();
-        move_rows<HD>(a.c, layer, list, count);
+        u32x4 xv[U], xk[U];
+        float xm[MOVE / NT + 1];
+        auto fetch = [&](int p) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int e = tid + u * NT, row = p * ROWS + e / (HD / 8);
+                const uint32_t x = row < count ? list[row].x : NONE;
+                if (x != NONE) xk[u] = *reinterpret_cast<const u32x4 *>(k + (size_t)x * HD + e % (HD / 8) * 8);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int e = tid + u * NT;
+                const uint32_t x = from_tile[e / (DIMS * 4)];
+                if (x != NONE)
+                    xv[u] = *reinterpret_cast<const u32x4 *>(v + (size_t)x * HD + (p * DIMS + e / 4 % DIMS) * PAGED_TILE + e % 4 * 8);
+            }
+        };
+#pragma unroll
+        for (int u = 0; u < MOVE / NT + 1; ++u) {
+            const int i = tid + u * NT;
+            const uint32_t x = i < count ? list[i].x : NONE;
+            if (x != NONE) xm[u] = mass[x];
+        }
+        fetch(0);
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int e = tid + u * NT;
+                uint2 *to = reinterpret_cast<uint2 *>(sm + e / 4 * V_DIM + e % 4 * 16);
+                to[0] = make_uint2(xv[u][0], xv[u][1]);
+                to[1] = make_uint2(xv[u][2], xv[u][3]);
+            }
+            // everything that this step's stores may overwrite has been read, by all waves
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int e = tid + u * NT, row = p * ROWS + e / (HD / 8);
+                const uint32_t y = row < count ? list[row].y : NONE;
+                if (y != NONE) *reinterpret_cast<u32x4 *>(k + (size_t)y * HD + e % (HD / 8) * 8) = xk[u];
+            }
+            if (p + 1 < PASSES) fetch(p + 1);
+            if (p == 0)
+#pragma unroll
+                for (int u = 0; u < MOVE / NT + 1; ++u) {
+                    const int i = tid + u * NT;
+                    const uint32_t y = i < count ? list[i].y : NONE;
+                    if (y != NONE) mass[y] = xm[u];
+                }
+            for (int e = tid; e < ((done & 7) + count + 7) / 8 * DIMS; e += NT) {
+                const int dim = e % DIMS, c = e / DIMS, to = (done & ~7) + 8 * c;
+                const uint32_t y = to_tile[(to >> 5) - (done >> 5)];
+                if (y == NONE) continue;
+                uint16_t *at = v + (size_t)y * HD + (p * DIMS + dim) * PAGED_TILE + (to & 31);
+                const u32x4 o = *reinterpret_cast<const u32x4 *>(off + 8 * c);
+                uint32_t n[8];
+                bool all = true;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    n[i] = o[i / 2] >> (16 * (i & 1)) & 0xffff;
+                    all &= n[i] != 0xffff;
+                }
+                if (all) {
+                    u32x4 x;
+#pragma unroll
+                    for (int i = 0; i < 8; i += 2)
+                        x[i / 2] = *reinterpret_cast<const uint16_t *>(sm + n[i] + dim * V_DIM) |
+                                   (uint32_t)*reinterpret_cast<const uint16_t *>(sm + n[i + 1] + dim * V_DIM) << 16;
+                    *reinterpret_cast<u32x4 *>(at) = x;
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if (n[i] != 0xffff) at[i] = *reinterpret_cast<const uint16_t *>(sm + n[i] + dim * V_DIM);
+                }
+            }
+            __syncthreads();
+        }
         done += count;
-        __syncthreads();
     }
     report(a.c, bad);
 }
@@ -1160,8 +1280,11 @@ hipError_t launch_paged_commit(const PagedMoveArgs &a, hipStream_t s)
 hipError_t launch_paged_evict(const PagedMoveArgs &a, hipStream_t s)
 {
     const unsigned units = (unsigned)a.c.L * a.c.n_seqs * a.c.H;
-    const size_t bits = ((size_t)a.c.width * a.c.page + 31) / 32 * 4;
-    a.c.hd == 64 ? k_paged_evict<64><<<units, 512, bits, s>>>(a) : k_paged_evict<128><<<units, 512, bits, s>>>(a);
+    const size_t slots = (size_t)a.c.width * a.c.page;
+    if (slots <= PAGED_MAX_RANKS)
+        a.c.hd == 64 ? k_paged_evict<64, true><<<units, 512, slots / 8, s>>>(a) : k_paged_evict<128, true><<<units, 512, slots / 8, s>>>(a);
+    else
+        a.c.hd == 64 ? k_paged_evict<64, false><<<units, 512, slots / 8, s>>>(a) : k_paged_evict<128, false><<<units, 512, slots / 8, s>>>(a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.new_lens != a.c.lens) return e;
     k_paged_evict_lens<<<(a.c.n_seqs + 255) / 256, 256, 0, s>>>(a);

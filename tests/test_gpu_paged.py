@@ -709,6 +709,27 @@ def test_evict_long(n, budget, recent):
     _check_evict(c, budget, recent)
 
 
+@pytest.mark.parametrize("width", [400, 321, 4096])
+def test_evict_from_wide_tables(width):
+    """Tables of more slots than the ranks that fit LDS, up to the widest."""
+    c = Case(width, [3001, 10, 900], [0, 0, 0], hd=64, heads=2, page=64, layers=1)
+    table = torch.full((3, width), -1, dtype=torch.int32, device=DEV)
+    table[:, :c.g.table.shape[1]] = c.g.table
+    c.g.table, c.g.c.table, c.g.c.table_stride = table, table.data_ptr(), width
+    _check_evict(c, 800, 64)
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_evict_with_runs(hd):
+    """Long runs that stay and go: tiles without a slot, whole ones, batches that begin inside a store."""
+    c = Case(83, [2400, 1700], [0, 0], hd=hd, heads=2, page=96, layers=2)
+    for i, pages in enumerate(c.pages):
+        for s, (p, at) in enumerate(c.o.places(pages, range(c.lens[i]))):
+            c.o.mass[:, p, :, at] = (1 if (s // 333) % 2 == i else 0) + np.float32(c.rng.random(c.o.mass[:, p, :, at].shape)) * (s % 50 == 7)
+    c.upload()
+    _check_evict(c, 1003, 21)
+
+
 def test_ties_go_to_the_lower_slot():
     """Few different masses, the zeros of both signs, NaN, infinities, the smallest and the largest."""
     c = Case(80, [700, 90], [0, 0], hd=64, heads=3, page=32, layers=2)
