@@ -193,6 +193,8 @@ int dv_paged_append(const dv_paged *c, int32_t layer, const dv_paged_rows *r, co
         return set_err(nullptr, DV_EINVAL, "rot_dim %d is odd or outside [2, %d]", rope->rot_dim, c->head_dim);
     if (rope && (!(rope->magnitude > 0.) || !std::isfinite((float)rope->magnitude)))
         return set_err(nullptr, DV_EINVAL, "bad magnitude %g", rope->magnitude);
+    if ((int64_t)r->n_rows * ((r->q ? r->n_heads : 0) + 2 * (int64_t)c->n_heads + 32) > 16 * MAX_GROUPS)
+        return set_err(nullptr, DV_EINVAL, "%d rows of %d heads are too many for one call", r->n_rows, r->n_heads);
     PagedAppendArgs a{};
     a.c = view_of(c, layer);
     a.start = r->start;

@@ -226,6 +226,13 @@ template <int N, typename F> __device__ __forceinline__ void each(F f)
 // * freq.  Angles are reduced in 64 bits (a position of 10^6 times a frequency of 1 leaves
 // fp32 seven bits behind the point); sin and cos are those of the angle's fp32 number with the
 // rest as a first-order term; products and sums are fp32, and a result is rounded once.
+//
+// Two ways, by the rows per sequence.  Few (decoding, small trees): a workgroup has 16 or 32 heads of a row, one
+// load and one store each; what bounds it is V, where each number of a new slot is 2 bytes of a line of its
+// own (64 rows of 40 + 40 + 40 heads: 8.2 us; with the rows and not the head groups as the grid's slow dimension
+// 12.8).  Many (8 rows a sequence and more): all heads of 4 rows, so that a row's place and turns are found once, and
+// V by way of LDS (6124 rows of 32 + 8 + 8 heads, bf16, 90 MB: 29 us, 3.1 TB/s; a workgroup for 16 heads of a row
+// 37; the values' workgroups ahead of the others 34).
 
 // cos and sin of angle, times m
 __device__ __forceinline__ float2 turn_of(double angle, float m)
@@ -254,14 +261,172 @@ __device__ __forceinline__ int seq_of_row(const int32_t *start, int n_seqs, int 
     return lo;
 }
 
-// Workgroup (row, group of heads): 8 dims of a head per thread.
+// The values of 32 rows and one KV head: V's slots are its fastest dimension, so the rows are turned
+// over in LDS, and 8 that stand in 8 aligned slots are one store per dim.
+constexpr int V_ROWS = 32;
+template <bool BF, int HD> __device__ __forceinline__ void append_values(const PagedAppendArgs &a, int row0, int h)
+{
+    constexpr int LD = HD + 8;
+    __shared__ __align__(16) uint16_t sm_v[V_ROWS][LD];
+    __shared__ uint32_t sm_row[V_ROWS];
+    const int tid = threadIdx.x;
+    constexpr int U = V_ROWS * (HD / 8) / 256;
+    float x[U][8];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int e = tid + u * 256, row = row0 + e / (HD / 8);
+        if (row < a.n_rows) load8<BF>(a.v, row * a.ldv + (int64_t)h * HD + e % (HD / 8) * 8, x[u]);
+    }
+    if (tid < 64) {
+        bool bad = false;
+        int s = a.start ? seq_of_row(a.start, a.c.n_seqs, row0) : 0;
+        const int row = row0 + tid;
+        if (tid < V_ROWS) {
+            if (a.start)
+                while (s < a.c.n_seqs && a.start[s + 1] <= row) ++s;
+            else
+                s = row;
+            sm_row[tid] = NONE;
+            if (row < a.n_rows && s < a.c.n_seqs) {
+                const Seq q = seq_of(a.c, a.start, a.n_rows, s, 1 << 30, bad);
+                if (row >= q.first && row - q.first < q.n) sm_row[tid] = row_of(a.c, s, h, q.len + row - q.first, bad);
+            }
+        }
+        report(a.c, bad);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const int e = tid + u * 256;
+        *reinterpret_cast<u32x4 *>(&sm_v[e / (HD / 8)][e % (HD / 8) * 8]) = bf16x8_of(x[u]);
+    }
+    __syncthreads();
+    for (int e = tid; e < V_ROWS * HD; e += 256) {
+        const int i = e / HD, d = e % HD;  // (i is the same in a wave)
+        const uint32_t r = sm_row[i];
+        if (r == NONE) continue;
+        uint16_t *to = a.c.v + ((size_t)(r / PAGED_TILE) * HD + d) * PAGED_TILE + r % PAGED_TILE;
+        // the first of the 8 aligned slots that r is among stands in row lead, if all 8 are here
+        const int lead = i - (int)(r % 8);
+        bool all = lead >= 0 && lead + 8 <= V_ROWS;
+#pragma unroll
+        for (int u = 0; u < 8; ++u) all = all && sm_row[lead + u] == r - r % 8 + u;
+        if (!all) {
+            *to = sm_v[i][d];
+        } else if (lead == i) {
+            u32x4 y;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) y[u] = sm_v[i + 2 * u][d] | (uint32_t)sm_v[i + 2 * u + 1][d] << 16;
+            *reinterpret_cast<u32x4 *>(to) = y;
+        }
+    }
+}
+
+// 8 dims of a head, from d0 on, turned; at: the head's numbers in LDS
+__device__ __forceinline__ void turn8(const PagedAppendArgs &a, const float *at, const float2 *turn, int d0, float (&x)[8])
+{
+    const int half = a.rot / 2;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int d = d0 + i;
+        if (d >= a.rot) break;
+        const bool second = a.interleaved ? d & 1 : d >= half;
+        const int pair = a.interleaved ? d >> 1 : second ? d - half : d;
+        const float y = at[a.interleaved ? d ^ 1 : second ? d - half : d + half];
+        const float2 t = turn[pair];
+        x[i] = fmaf(x[i], t.x, second ? y * t.y : -(y * t.y));
+    }
+}
+
+// The queries and keys of 4 rows, all heads: a wave finds a row's place and turns, then HD / 8 threads
+// have a head at a time and ask for the next one's numbers before they turn its.
+template <bool BF, int HD> __device__ __forceinline__ void append_rows(const PagedAppendArgs &a, int row0)
+{
+    constexpr int R = 4, PER = HD / 8, AT_ONCE = 256 / PER;
+    __shared__ float2 sm_turn[R][64];
+    __shared__ __align__(16) float sm_x[AT_ONCE][HD];
+    __shared__ uint32_t sm_row[R];  // of KV head 0
+    __shared__ bool sm_own[R];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, d0 = 8 * (tid % PER), heads = a.Hq + a.c.H, mine = tid / PER;
+    float x[8] = {};
+    auto fetch = [&](int it) {
+        const int i = (uint32_t)it / (uint32_t)heads, head = it - i * heads, row = row0 + i;
+        if (i >= R || row >= a.n_rows) return;
+        const bool is_q = head < a.Hq;
+        load8<BF>(is_q ? a.q : a.k, row * (is_q ? a.ldq : a.ldk) + (int64_t)(is_q ? head : head - a.Hq) * HD + d0, x);
+    };
+    fetch(mine);
+    {
+        const int row = row0 + wave;
+        bool own = false, bad = false;
+        uint32_t r = NONE;
+        if (row < a.n_rows) {
+            int pos = a.positions ? a.positions[row] : 0;
+            const int s = a.start ? seq_of_row(a.start, a.c.n_seqs, row) : row;
+            if (s < a.c.n_seqs) {
+                const Seq q = seq_of(a.c, a.start, a.n_rows, s, 1 << 30, bad);
+                own = row >= q.first && row - q.first < q.n;
+                if (own) {
+                    r = row_of(a.c, s, 0, q.len + row - q.first, bad);
+                    if (!a.positions) pos = q.len + row - q.first;
+                    if (lane < a.rot / 2) sm_turn[wave][lane] = turn_of(pos * a.freq[lane], a.magnitude);
+                }
+            }
+        }
+        if (lane == 0) {
+            sm_row[wave] = r;
+            sm_own[wave] = own;
+        }
+        report(a.c, bad);
+    }
+    __syncthreads();
+    for (int it = mine; it < R * heads; it += AT_ONCE) {
+        const int i = (uint32_t)it / (uint32_t)heads, head = it - i * heads;
+        float y[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] = x[j];
+#pragma unroll
+        for (int j = 0; j < 8; j += 4) *reinterpret_cast<float4 *>(&sm_x[mine][d0 + j]) = make_float4(y[j], y[j + 1], y[j + 2], y[j + 3]);
+        fetch(it + AT_ONCE);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // (a head's threads are of one wave)
+        if (sm_own[i]) {
+            turn8(a, sm_x[mine], sm_turn[i], d0, y);
+            if (head < a.Hq) {
+                store8<BF>(a.q, (row0 + i) * a.ldq + (int64_t)head * HD + d0, y);
+            } else if (sm_row[i] != NONE) {
+                const uint32_t r = sm_row[i] + (uint32_t)(head - a.Hq) * (uint32_t)a.c.page;
+                *reinterpret_cast<u32x4 *>(a.c.k + (size_t)r * HD + d0) = bf16x8_of(y);
+                if (d0 == 0 && a.c.mass) a.c.mass[r] = 0.f;
+            }
+        }
+        asm volatile("" ::: "memory");
+    }
+}
+
+// Many rows of a sequence: workgroups of 4 rows' queries and keys, behind them those of 32 rows' values.
+template <bool BF, int HD> __global__ __launch_bounds__(256) void k_paged_append_rows(PagedAppendArgs a)
+{
+    const int groups = (a.n_rows + 3) / 4, b = blockIdx.x - groups;
+    if (b < 0)
+        append_rows<BF, HD>(a, blockIdx.x * 4);
+    else
+        append_values<BF, HD>(a, b / a.c.H * V_ROWS, b % a.c.H);
+}
+
+// Few rows: workgroup (row, group of heads), 8 dims of a head per thread.
 template <bool BF, int HD> __global__ __launch_bounds__(256) void k_paged_append(PagedAppendArgs a)
 {
     constexpr int PER = HD / 8, HEADS = 256 / PER;
     __shared__ float2 sm_turn[64];
-    __shared__ float sm_x[HEADS][HD];
-    const int row = blockIdx.x, tid = threadIdx.x, d0 = 8 * (tid % PER);
-    const int head = blockIdx.y * HEADS + tid / PER, kv = head - a.Hq, H = a.c.H;
+    __shared__ __align__(16) float sm_x[HEADS][HD];
+    const int tid = threadIdx.x, d0 = 8 * (tid % PER), H = a.c.H;
+    const int row = blockIdx.x, heads = a.Hq + 2 * H, head = blockIdx.y * HEADS + tid / PER, kv = head - a.Hq;
+    // (asked for first: nothing else is needed for these)
+    const bool there = head < heads, is_q = kv < 0, is_k = !is_q && kv < H;
+    int pos = a.positions ? a.positions[row] : 0;
+    float x[8] = {};
+    if (there)
+        load8<BF>(is_q ? a.q : is_k ? a.k : a.v,
+                  row * (is_q ? a.ldq : is_k ? a.ldk : a.ldv) + (int64_t)(is_q ? head : is_k ? kv : kv - H) * HD + d0, x);
     const int s = a.start ? seq_of_row(a.start, a.c.n_seqs, row) : row;
     if (s >= a.c.n_seqs) return;
     bool bad = false;
@@ -271,40 +436,22 @@ template <bool BF, int HD> __global__ __launch_bounds__(256) void k_paged_append
         return;
     }
     const int slot = q.len + row - q.first;
-    if (tid < a.rot / 2) sm_turn[tid] = turn_of((a.positions ? a.positions[row] : slot) * a.freq[tid], a.magnitude);
-    const bool there = head < a.Hq + 2 * H;
-    float x[8] = {};
-    if (there) {
-        const bool is_q = kv < 0, is_k = kv < H;
-        load8<BF>(is_q ? a.q : is_k ? a.k : a.v,
-                  row * (is_q ? a.ldq : is_k ? a.ldk : a.ldv) + (int64_t)(is_q ? head : is_k ? kv : kv - H) * HD + d0, x);
+    if (!a.positions) pos = slot;
+    const uint32_t r = there && !is_q ? row_of(a.c, s, is_k ? kv : kv - H, slot, bad) : NONE;
+    if (tid < a.rot / 2) sm_turn[tid] = turn_of(pos * a.freq[tid], a.magnitude);
+    if (there && (is_q || is_k))
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sm_x[tid / PER][d0 + i] = x[i];
-    }
+        for (int i = 0; i < 8; i += 4) *reinterpret_cast<float4 *>(&sm_x[tid / PER][d0 + i]) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
     __syncthreads();
-    if (!there) return;
-    if (kv < H) {
-        const int half = a.rot / 2;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int d = d0 + i;
-            if (d >= a.rot) break;
-            const bool second = a.interleaved ? d & 1 : d >= half;
-            const int pair = a.interleaved ? d >> 1 : second ? d - half : d;
-            const float y = sm_x[tid / PER][a.interleaved ? d ^ 1 : second ? d - half : d + half];
-            const float2 t = sm_turn[pair];
-            x[i] = fmaf(x[i], t.x, second ? y * t.y : -(y * t.y));
-        }
-        if (kv < 0) {
-            store8<BF>(a.q, row * a.ldq + (int64_t)head * HD + d0, x);
-            return;
-        }
-    }
-    const int h = kv < H ? kv : kv - H;
-    const uint32_t r = row_of(a.c, s, h, slot, bad);
     report(a.c, bad);
+    if (!there) return;
+    if (is_q || is_k) turn8(a, sm_x[tid / PER], sm_turn, d0, x);
+    if (is_q) {
+        store8<BF>(a.q, row * a.ldq + (int64_t)head * HD + d0, x);
+        return;
+    }
     if (r == NONE) return;
-    if (kv < H) {
+    if (is_k) {
         *reinterpret_cast<u32x4 *>(a.c.k + (size_t)r * HD + d0) = bf16x8_of(x);
         if (d0 == 0 && a.c.mass) a.c.mass[r] = 0.f;
     } else {
@@ -756,7 +903,9 @@ template <int HD, bool BF, int RT, int NW, int LANES> __global__ __launch_bounds
 // ---------------------------------------------------------------------------
 // Mass: mass_j += sum over counted rows of exp(z_ij - m_i) / l_i.  The scores are made again
 // from K alone, half of what attention read; a tile belongs to one wave, which adds its
-// rows in order, so nothing is atomic.
+// rows in order, so nothing is atomic.  A tile's masses are asked for with its keys: read where they are added to, they
+// hold up the keys behind them (loads return in order; 29 us for 37 of 16 ragged sequences, 4 rows a KV head).
+// Now 21.8 us for those (80 MB, 3.7 TB/s), 28.6 for two of up to 8191 slots with 16 fp32 rows of 32 heads (98 MB).
 
 // Sum over the 16 lanes of a row of lanes, in all of them: rotations inside the row
 __device__ __forceinline__ float row_sum(float x)
@@ -854,7 +1003,8 @@ template <int HD, bool BF> __global__ __launch_bounds__(512) void k_paged_mass(P
 // Commit moves rows of a (layer, sequence, KV head) to lower slots, in order.  Source slots increase, and
 // each is at least its destination; so a wave that always has the same columns of K (or dims of V) can
 // go through the list by itself: what it overwrites is no later row's source, and a step's loads stand before
-// its stores.
+// its stores.  What bounds it is V, whose lines hold 32 slots of a dim: five rows of 8 sequences, 40 layers
+// of 40 heads 70 us (63 MB of rows, about 300 of lines), 38 of 16 sequences, 32 of 32, 124 (501 MB, 4.0 TB/s).
 
 // Rows list[i].x to list[i].y, i < count; NONE in either: not moved.  8 waves.
 template <int HD> __device__ __forceinline__ void move_rows(const PagedView &c, int layer, const uint2 *list, int count)
@@ -956,6 +1106,10 @@ __global__ __launch_bounds__(256) void k_paged_commit_lens(PagedMoveArgs a)
 // of V, whose slots are its fastest dimension, 32 dims of all 24 tiles are laid into LDS and
 // gathered there, 8 slots of a dim to a store.  Source slots increase and each is at least its
 // destination: what a step overwrites is in registers or LDS by then, and no later step's source.
+// What bounds it is that V's tiles are read whole for the slots that stay, and the rate of one CU where heads are few:
+// 128 heads, 2049 slots to 1024 62 us (1.3 MB a workgroup at 26 GB/s, 10 us before the first row moves);
+// 16 ragged sequences of up to 4500 slots to 1500, 64 heads and layers, 406 us (about 1.6 GB).  With V gathered 2 bytes a
+// lane from memory 73 and 460; with ranks read from memory in each of the five passes as well 76 and 528.
 
 constexpr int MOVE_TILES = 24, MOVE = MOVE_TILES * PAGED_TILE, DIMS = 32, V_DIM = 72;  // V_DIM: bytes of a dim's tile in LDS
 
@@ -1205,7 +1359,10 @@ __global__ __launch_bounds__(256) void k_paged_evict_lens(PagedMoveArgs a)
 template <bool BF, int HD> void append(const PagedAppendArgs &a, hipStream_t s)
 {
     constexpr int HEADS = 256 / (HD / 8);
-    k_paged_append<BF, HD><<<dim3(a.n_rows, (a.Hq + 2 * a.c.H + HEADS - 1) / HEADS), 256, 0, s>>>(a);
+    if (a.n_rows >= 8ll * a.c.n_seqs)
+        k_paged_append_rows<BF, HD><<<(a.n_rows + 3) / 4 + (a.n_rows + V_ROWS - 1) / V_ROWS * a.c.H, 256, 0, s>>>(a);
+    else
+        k_paged_append<BF, HD><<<dim3(a.n_rows, (a.Hq + 2 * a.c.H + HEADS - 1) / HEADS), 256, 0, s>>>(a);
 }
 
 template <int HD, bool BF, int RT, int NW> void attention(const PagedAttnArgs &a, const PagedCut &cut, hipStream_t s)
