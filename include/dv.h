@@ -464,7 +464,7 @@ typedef struct dv_paged {
  *     (rows of 16-byte alignment, at least n_heads head_dim).  n_heads is a multiple of the cache's,
  *     at most 1024 times as many: query heads h with the same h / (n_heads / pg->n_heads) share
  *     a KV head;
- *   start: device int32 [n_seqs + 1], not decreasing; rows from start[n_seqs] on belong to nobody
+ *   start: device int32 [n_seqs + 1], not decreasing (no row has two sequences); rows from start[n_seqs] on belong to nobody
  *     and are left as they are.  NULL: one row per sequence, n_rows = n_seqs.  n_rows is at most 2^22;
  *   mask:  device uint64 [n_rows]: bit j of a row: it sees new row j of its sequence (dv_tree_prepare's
  *     out_anc).  NULL: new row i sees rows 0..i.  Committed slots are always seen;

@@ -268,7 +268,9 @@ int dv_paged_mass(const dv_paged *c, int32_t layer, const dv_paged_rows *r, cons
     a.r = view_of(c, r);
     a.stats = reinterpret_cast<const float2 *>(stats);
     a.count = count;
-    a.groups = paged_mass_groups(c->n_seqs, c->n_heads, r->max_len, n_cu);
+    const PagedMassCut cut = paged_mass_cut(c->n_seqs, c->n_heads, r->max_len, n_cu);
+    a.whole = cut.whole;
+    a.groups = (int)cut.grid;
     return launched(launch_paged_mass(a, r->dtype == DV_BF16, static_cast<hipStream_t>(stream)), "mass");
 }
 

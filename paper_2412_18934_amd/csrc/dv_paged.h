@@ -9,6 +9,7 @@
 
 #define PAGED_TILE 32        // slots of a V tile, and of a step of attention
 #define PAGED_MAX_NEW 64     // new rows of a sequence that a mask names
+#define PAGED_MAX_LINE 1024    // sequences among which a workgroup looks for its piece (64 at a time, about 1 us)
 #define PAGED_MAX_PIECES (1 << 20)
 #define PAGED_MAX_RANKS 10240   // slots of a sequence whose ranks an eviction keeps in LDS
 #define PAGED_MAX_EVICT 262144  // slots of a sequence that an eviction marks in LDS, a bit each
@@ -83,7 +84,7 @@ inline PagedCut paged_cut(int n_seqs, int heads, int group, int n_rows, int max_
     const int block = 16 * c.rt;
     c.blocks = (int)((rows + block - 1) / block);
     const int64_t units = (int64_t)n_seqs * heads * c.blocks, limit = units >= 2 * slots ? 96 : 48;
-    c.whole = tiles <= (16 + units / 4 < limit ? 16 + units / 4 : limit);
+    c.whole = tiles <= (16 + units / 4 < limit ? 16 + units / 4 : limit) || n_seqs > PAGED_MAX_LINE;
     // units of any rows: a sequence has at most 64, and all together n_rows
     const int64_t most = ((int64_t)PAGED_MAX_NEW * group + block - 1) / block * n_seqs, sum = (int64_t)n_rows * group / block + n_seqs;
     const int64_t bound = heads * (most < sum ? most : sum);
@@ -97,12 +98,16 @@ inline size_t paged_attention_bytes(const PagedCut &c, int hd)
     return c.whole ? 0 : (size_t)c.groups * 16 * c.rt * (hd + 2) * 4;
 }
 
-// Workgroups that share mass's tiles
-inline int paged_mass_groups(int n_seqs, int heads, int max_len, int n_cu)
+// Mass: a workgroup per sequence and KV head where these are many, else pieces as above.
+struct PagedMassCut {
+    bool whole;
+    int64_t grid;
+};
+inline PagedMassCut paged_mass_cut(int n_seqs, int heads, int max_len, int n_cu)
 {
-    const int64_t units = (int64_t)n_seqs * heads, most = (units * (max_len / PAGED_TILE + 1) + 7) / 8;
-    const int64_t groups = most < 2 * n_cu ? most : 2 * n_cu;
-    return (int)(groups > units ? groups : units);
+    const int64_t units = (int64_t)n_seqs * heads, slots = 2 * n_cu, most = (units * (max_len / PAGED_TILE + 1) + 7) / 8;
+    const int64_t pieces = most < slots ? most : slots;
+    return {units >= 8 * slots || n_seqs > PAGED_MAX_LINE, pieces > units ? pieces : units};
 }
 
 struct PagedMassArgs {
@@ -110,7 +115,7 @@ struct PagedMassArgs {
     PagedRowsView r;
     const float2 *stats;
     const uint64_t *count;
-    int32_t groups;
+    int32_t whole, groups;  // groups: workgroups
 };
 
 struct PagedMoveArgs {

@@ -995,7 +995,13 @@ template <int HD, bool BF> __global__ __launch_bounds__(512) void k_paged_mass(P
     };
 
     Segment x;
-    if (piece_at(a.c, a.r, 1 << 30, gridDim.x, NW, blockIdx.x, x, bad)) segment(x.q, x.s, x.h, x.t0, x.t1);
+    if (a.whole) {
+        const int s = blockIdx.x / a.c.H;
+        const Seq q = seq_of(a.c, a.r.start, a.r.n_rows, s, PAGED_MAX_NEW, bad);
+        segment(q, s, blockIdx.x % a.c.H, 0, load_of(a.c, q, a.r.G, 1 << 30).tiles);
+    } else if (piece_at(a.c, a.r, 1 << 30, gridDim.x, NW, blockIdx.x, x, bad)) {
+        segment(x.q, x.s, x.h, x.t0, x.t1);
+    }
     report(a.c, bad);
 }
 
@@ -1004,15 +1010,17 @@ template <int HD, bool BF> __global__ __launch_bounds__(512) void k_paged_mass(P
 // each is at least its destination; so a wave that always has the same columns of K (or dims of V) can
 // go through the list by itself: what it overwrites is no later row's source, and a step's loads stand before
 // its stores.  What bounds it is V, whose lines hold 32 slots of a dim: five rows of 8 sequences, 40 layers
-// of 40 heads 70 us (63 MB of rows, about 300 of lines), 38 of 16 sequences, 32 of 32, 124 (501 MB, 4.0 TB/s).
+// of 40 heads 48 us (63 MB of rows, about 300 of lines), 38 of 16 sequences, 32 of 32, 114 (501 MB, 4.4 TB/s).
+// Workgroups are small, so that many wait for their chain of lengths, path, table and rows at once: 4 waves
+// 52 and 112, 8 waves 70 and 124.
 
-// Rows list[i].x to list[i].y, i < count; NONE in either: not moved.  8 waves.
-template <int HD> __device__ __forceinline__ void move_rows(const PagedView &c, int layer, const uint2 *list, int count)
+// Rows list[i].x to list[i].y, i < count; NONE in either: not moved.  NW waves.
+template <int HD, int NW> __device__ __forceinline__ void move_rows(const PagedView &c, int layer, const uint2 *list, int count)
 {
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const size_t base = (size_t)layer * c.n_pages * c.H * c.page;
-    if (wave < 4) {  // K: a quarter of the columns
-        constexpr int CH = HD / 32, ROWS = 64 / CH, U = 8;  // 16 bytes each
+    if (wave < NW / 2) {  // K: a share of the columns
+        constexpr int CH = HD / 4 / NW, ROWS = 64 / CH, U = 4;  // 16 bytes each
         uint16_t *k = c.k + base * HD + (wave * CH + lane % CH) * 8;
         for (int i0 = 0; i0 < count; i0 += ROWS * U) {
             u32x4 x[U];
@@ -1037,33 +1045,24 @@ template <int HD> __device__ __forceinline__ void move_rows(const PagedView &c, 
                 mass[e.y] = m;
             }
         }
-    } else {  // V: a quarter of the dims, two of them and 32 rows a load
-        constexpr int U = HD / 8, T = 2;
-        uint16_t *v = c.v + base * HD + ((wave - 4) * (HD / 4) + lane / 32) * PAGED_TILE;
-        for (int i0 = 0; i0 < count; i0 += 32 * T) {
-            uint16_t x[T][U], *to[T];
-            bool moves[T];
+    } else {  // V: a share of the dims, two of them and 32 rows a load
+        constexpr int U = HD / NW;
+        uint16_t *v = c.v + base * HD + ((wave - NW / 2) * (2 * HD / NW) + lane / 32) * PAGED_TILE;
+        for (int i0 = 0; i0 < count; i0 += 32) {
+            const int i = i0 + lane % 32;
+            const uint2 e = i < count ? list[i] : make_uint2(NONE, NONE);
+            if (e.x == NONE || e.y == NONE) continue;
+            uint16_t x[U], *to = v + (size_t)(e.y / PAGED_TILE) * HD * PAGED_TILE + e.y % PAGED_TILE;
+            const uint16_t *from = v + (size_t)(e.x / PAGED_TILE) * HD * PAGED_TILE + e.x % PAGED_TILE;
 #pragma unroll
-            for (int t = 0; t < T; ++t) {
-                const int i = i0 + 32 * t + lane % 32;
-                const uint2 e = i < count ? list[i] : make_uint2(NONE, NONE);
-                moves[t] = e.x != NONE && e.y != NONE;
-                to[t] = v + (size_t)(e.y / PAGED_TILE) * HD * PAGED_TILE + e.y % PAGED_TILE;
-                const uint16_t *from = v + (size_t)(e.x / PAGED_TILE) * HD * PAGED_TILE + e.x % PAGED_TILE;
-                if (moves[t])
+            for (int u = 0; u < U; ++u) x[u] = from[2 * u * PAGED_TILE];
 #pragma unroll
-                    for (int u = 0; u < U; ++u) x[t][u] = from[2 * u * PAGED_TILE];
-            }
-#pragma unroll
-            for (int t = 0; t < T; ++t)
-                if (moves[t])
-#pragma unroll
-                    for (int u = 0; u < U; ++u) to[t][2 * u * PAGED_TILE] = x[t][u];
+            for (int u = 0; u < U; ++u) to[2 * u * PAGED_TILE] = x[u];
         }
     }
 }
 
-template <int HD> __global__ __launch_bounds__(512) void k_paged_commit(PagedMoveArgs a)
+template <int HD, int NW> __global__ __launch_bounds__(64 * NW) void k_paged_commit(PagedMoveArgs a)
 {
     __shared__ uint2 list[PAGED_MAX_NEW];
     const int h = blockIdx.x % a.c.H, s = blockIdx.x / a.c.H % a.c.n_seqs, layer = blockIdx.x / a.c.H / a.c.n_seqs;
@@ -1084,7 +1083,7 @@ template <int HD> __global__ __launch_bounds__(512) void k_paged_commit(PagedMov
     }
     __syncthreads();
     report(a.c, bad);
-    move_rows<HD>(a.c, layer, list, n);
+    move_rows<HD, NW>(a.c, layer, list, n);
 }
 
 __global__ __launch_bounds__(256) void k_paged_commit_lens(PagedMoveArgs a)
@@ -1426,7 +1425,7 @@ hipError_t launch_paged_commit(const PagedMoveArgs &a, hipStream_t s)
 {
     if (a.path) {
         const unsigned units = (unsigned)a.c.L * a.c.n_seqs * a.c.H;
-        a.c.hd == 64 ? k_paged_commit<64><<<units, 512, 0, s>>>(a) : k_paged_commit<128><<<units, 512, 0, s>>>(a);
+        a.c.hd == 64 ? k_paged_commit<64, 2><<<units, 128, 0, s>>>(a) : k_paged_commit<128, 2><<<units, 128, 0, s>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess || a.new_lens != a.c.lens) return e;
     }

@@ -590,6 +590,19 @@ def test_mass_of_counted_rows(max_len):
     _check_mass(c, counts, 5, "f32", "tree", counted=[0b10010000000000000101, 0, 1, 2 ** 64 - 1], max_len=max_len)
 
 
+@pytest.mark.parametrize("seqs,length,max_len", [(90, 100, 100000), (300, 70, 100000), (1100, 40, 100000)])
+def test_many_sequences(seqs, length, max_len):
+    """More than a wave's lanes, and more than a workgroup looks through: attention and mass."""
+    rng = np.random.default_rng(seqs)
+    lens = [int(x) for x in rng.integers(0, length, seqs)]
+    counts = [int(x) for x in rng.integers(0, 3, seqs)]
+    counts[-1] = 2
+    c = Case(seqs, lens, counts, heads=1, hd=64, page=32, layers=1)
+    c.put_new(0, counts)
+    _check_attention(c, counts, 2, "bf16", "chain", layer=0, max_len=max_len)
+    _check_mass(c, counts, 2, "f32", "chain", layer=0, max_len=max_len, pad=2)
+
+
 def test_rows_that_do_not_count_may_be_anything():
     lens, counts = [40], [4]
     c = Case(72, lens, counts)

@@ -209,7 +209,7 @@ void t_cut(int seqs, int heads, int group, int n_rows, int rows, int len, int cu
 {
     const PagedCut c = paged_cut(seqs, heads, group, n_rows, rows, len, cu);
     out[0] = c.rt, out[1] = c.blocks, out[2] = c.groups, out[3] = c.whole, out[4] = (int64_t)paged_attention_bytes(c, 128);
-    out[5] = c.grid, out[6] = paged_mass_groups(seqs, heads, len, cu);
+    out[5] = c.grid, out[6] = paged_mass_cut(seqs, heads, len, cu).grid;
 }
 }
 """
