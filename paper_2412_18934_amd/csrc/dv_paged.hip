@@ -231,7 +231,7 @@ template <int N, typename F> __device__ __forceinline__ void each(F f)
 // load and one store each; what bounds it is V, where each number of a new slot is 2 bytes of a line of its
 // own (64 rows of 40 + 40 + 40 heads: 8.2 us; with the rows and not the head groups as the grid's slow dimension
 // 12.8).  Many (8 rows a sequence and more): all heads of 4 rows, so that a row's place and turns are found once, and
-// V by way of LDS (6124 rows of 32 + 8 + 8 heads, bf16, 90 MB: 29 us, 3.1 TB/s; a workgroup for 16 heads of a row
+// V by way of LDS (3800 rows of 32 + 8 + 8 heads, bf16, 90 MB: 28.6 us, 3.1 TB/s; a workgroup for 16 heads of a row
 // 37; the values' workgroups ahead of the others 34).
 
 // cos and sin of angle, times m
@@ -321,19 +321,47 @@ template <bool BF, int HD> __device__ __forceinline__ void append_values(const P
     }
 }
 
-// 8 dims of a head, from d0 on, turned; at: the head's numbers in LDS
+// 8 dims of a head, from d0 on, turned.  at: the head's numbers in LDS, needed where pairs are half a turn
+// apart (they are read in fours where the halves begin at a multiple of 8: one by one costs 8 conflicts a read).
 __device__ __forceinline__ void turn8(const PagedAppendArgs &a, const float *at, const float2 *turn, int d0, float (&x)[8])
 {
+    if (d0 >= a.rot) return;
     const int half = a.rot / 2;
+    if (a.interleaved) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int d = d0 + i;
-        if (d >= a.rot) break;
-        const bool second = a.interleaved ? d & 1 : d >= half;
-        const int pair = a.interleaved ? d >> 1 : second ? d - half : d;
-        const float y = at[a.interleaved ? d ^ 1 : second ? d - half : d + half];
-        const float2 t = turn[pair];
-        x[i] = fmaf(x[i], t.x, second ? y * t.y : -(y * t.y));
+        for (int i = 0; i < 8; i += 2) {
+            if (d0 + i >= a.rot) break;
+            const float2 t = turn[(d0 + i) / 2];
+            const float u = x[i], w = x[i + 1];
+            x[i] = fmaf(u, t.x, -(w * t.y));
+            x[i + 1] = fmaf(w, t.x, u * t.y);
+        }
+    } else if (half % 8 == 0) {
+        const bool second = d0 >= half;
+        const float *other = at + (second ? d0 - half : d0 + half);
+        const float4 *t4 = reinterpret_cast<const float4 *>(turn + (second ? d0 - half : d0));
+        float y[8];
+#pragma unroll
+        for (int i = 0; i < 8; i += 4) {
+            const float4 o = *reinterpret_cast<const float4 *>(other + i);
+            y[i] = o.x, y[i + 1] = o.y, y[i + 2] = o.z, y[i + 3] = o.w;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; i += 2) {
+            const float4 t = t4[i / 2];
+            x[i] = fmaf(x[i], t.x, second ? y[i] * t.y : -(y[i] * t.y));
+            x[i + 1] = fmaf(x[i + 1], t.z, second ? y[i + 1] * t.w : -(y[i + 1] * t.w));
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int d = d0 + i;
+            if (d >= a.rot) break;
+            const bool second = d >= half;
+            const float y = at[second ? d - half : d + half];
+            const float2 t = turn[second ? d - half : d];
+            x[i] = fmaf(x[i], t.x, second ? y * t.y : -(y * t.y));
+        }
     }
 }
 
@@ -342,7 +370,7 @@ __device__ __forceinline__ void turn8(const PagedAppendArgs &a, const float *at,
 template <bool BF, int HD> __device__ __forceinline__ void append_rows(const PagedAppendArgs &a, int row0)
 {
     constexpr int R = 4, PER = HD / 8, AT_ONCE = 256 / PER;
-    __shared__ float2 sm_turn[R][64];
+    __shared__ __align__(16) float2 sm_turn[R][64];
     __shared__ __align__(16) float sm_x[AT_ONCE][HD];
     __shared__ uint32_t sm_row[R];  // of KV head 0
     __shared__ bool sm_own[R];
@@ -416,7 +444,7 @@ template <bool BF, int HD> __global__ __launch_bounds__(256) void k_paged_append
 template <bool BF, int HD> __global__ __launch_bounds__(256) void k_paged_append(PagedAppendArgs a)
 {
     constexpr int PER = HD / 8, HEADS = 256 / PER;
-    __shared__ float2 sm_turn[64];
+    __shared__ __align__(16) float2 sm_turn[64];
     __shared__ __align__(16) float sm_x[HEADS][HD];
     const int tid = threadIdx.x, d0 = 8 * (tid % PER), H = a.c.H;
     const int row = blockIdx.x, heads = a.Hq + 2 * H, head = blockIdx.y * HEADS + tid / PER, kv = head - a.Hq;
