@@ -231,8 +231,8 @@ template <int N, typename F> __device__ __forceinline__ void each(F f)
 // load and one store each; what bounds it is V, where each number of a new slot is 2 bytes of a line of its
 // own (64 rows of 40 + 40 + 40 heads: 8.2 us; with the rows and not the head groups as the grid's slow dimension
 // 12.8).  Many (8 rows a sequence and more): all heads of 4 rows, so that a row's place and turns are found once, and
-// V by way of LDS (3800 rows of 32 + 8 + 8 heads, bf16, 90 MB: 28.6 us, 3.1 TB/s; a workgroup for 16 heads of a row
-// 37; the values' workgroups ahead of the others 34).
+// V by way of LDS (3800 rows of 32 + 8 + 8 heads, bf16, 90 MB: 22.3 us, 4.0 TB/s; a workgroup for 16 heads of a row
+// 37; the values' workgroups ahead of the others, or in turn with them, 5 to 7 more).
 
 // cos and sin of angle, times m
 __device__ __forceinline__ float2 turn_of(double angle, float m)
@@ -269,6 +269,7 @@ template <bool BF, int HD> __device__ __forceinline__ void append_values(const P
     constexpr int LD = HD + 8;
     __shared__ __align__(16) uint16_t sm_v[V_ROWS][LD];
     __shared__ uint32_t sm_row[V_ROWS];
+    __shared__ uint8_t sm_kind[V_ROWS];  // 0: nothing to store, 1: a number per dim, 8: eight, of the rows from here on
     const int tid = threadIdx.x;
     constexpr int U = V_ROWS * (HD / 8) / 256;
     float x[U][8];
@@ -300,19 +301,24 @@ template <bool BF, int HD> __device__ __forceinline__ void append_values(const P
         *reinterpret_cast<u32x4 *>(&sm_v[e / (HD / 8)][e % (HD / 8) * 8]) = bf16x8_of(x[u]);
     }
     __syncthreads();
-    for (int e = tid; e < V_ROWS * HD; e += 256) {
-        const int i = e / HD, d = e % HD;  // (i is the same in a wave)
-        const uint32_t r = sm_row[i];
-        if (r == NONE) continue;
-        uint16_t *to = a.c.v + ((size_t)(r / PAGED_TILE) * HD + d) * PAGED_TILE + r % PAGED_TILE;
-        // the first of the 8 aligned slots that r is among stands in row lead, if all 8 are here
-        const int lead = i - (int)(r % 8);
+    if (tid < V_ROWS) {
+        // the first of the 8 aligned slots that a row is among stands in row lead, if all 8 are here
+        const uint32_t r = sm_row[tid];
+        const int lead = tid - (int)(r % 8);
         bool all = lead >= 0 && lead + 8 <= V_ROWS;
 #pragma unroll
         for (int u = 0; u < 8; ++u) all = all && sm_row[lead + u] == r - r % 8 + u;
-        if (!all) {
+        sm_kind[tid] = r == NONE ? 0 : !all ? 1 : lead == tid ? 8 : 0;
+    }
+    __syncthreads();
+    for (int e = tid; e < V_ROWS * HD; e += 256) {
+        const int i = e / HD, d = e % HD, kind = sm_kind[i];  // (i is the same in a wave)
+        if (!kind) continue;
+        const uint32_t r = sm_row[i];
+        uint16_t *to = a.c.v + ((size_t)(r / PAGED_TILE) * HD + d) * PAGED_TILE + r % PAGED_TILE;
+        if (kind == 1) {
             *to = sm_v[i][d];
-        } else if (lead == i) {
+        } else {
             u32x4 y;
 #pragma unroll
             for (int u = 0; u < 4; ++u) y[u] = sm_v[i + 2 * u][d] | (uint32_t)sm_v[i + 2 * u + 1][d] << 16;
@@ -515,7 +521,8 @@ template <bool BF, int HD> __global__ __launch_bounds__(256) void k_paged_append
 // 41 us for eight 16-node trees); queries from LDS and not from 48 registers.
 // Not taken: equal shares of all tiles that run over units' ends (the eight trees 39 to 50 for 31 us: each end
 // costs a workgroup 4 us); 12 waves per CU (spills with fp32 rows, no gain with bf16); pieces in a loop per workgroup
-// (42 registers more).
+// (42 registers more); a whole tile ahead in registers of its own (96 for 90 us, 48 ragged sequences; 33 for 31, the
+// trees); a whole unit's first pages asked for before its length is known (no difference).
 
 // A 32-slot tile in registers, 16 bytes per lane and load
 template <int HD> struct Tile {
