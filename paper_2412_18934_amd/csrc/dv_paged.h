@@ -10,7 +10,6 @@
 #define PAGED_TILE 32        // slots of a V tile, and of a step of attention
 #define PAGED_MAX_NEW 64     // new rows of a sequence that a mask names
 #define PAGED_MAX_LINE 1024    // sequences among which a workgroup looks for its piece (64 at a time, about 1 us)
-#define PAGED_MAX_PIECES (1 << 20)
 #define PAGED_MAX_RANKS 10240   // slots of a sequence whose ranks an eviction keeps in LDS
 #define PAGED_MAX_EVICT 262144  // slots of a sequence that an eviction marks in LDS, a bit each
 
@@ -84,12 +83,13 @@ inline PagedCut paged_cut(int n_seqs, int heads, int group, int n_rows, int max_
     const int block = 16 * c.rt;
     c.blocks = (int)((rows + block - 1) / block);
     const int64_t units = (int64_t)n_seqs * heads * c.blocks, limit = units >= 2 * slots ? 96 : 48;
-    c.whole = tiles <= (16 + units / 4 < limit ? 16 + units / 4 : limit) || n_seqs > PAGED_MAX_LINE;
+    c.whole = tiles <= (16 + units / 4 < limit ? 16 + units / 4 : limit) || n_seqs > PAGED_MAX_LINE ||
+              units >= 8 * slots;  // (pieces of so many would be dozens of MB of sums, for the longest's sake)
     // units of any rows: a sequence has at most 64, and all together n_rows
     const int64_t most = ((int64_t)PAGED_MAX_NEW * group + block - 1) / block * n_seqs, sum = (int64_t)n_rows * group / block + n_seqs;
     const int64_t bound = heads * (most < sum ? most : sum);
     const int64_t pieces = units >= slots / 2 ? units + (c.rt == 1 ? slots : slots / 2) : slots;
-    c.groups = c.whole ? 0 : (int)(pieces < PAGED_MAX_PIECES ? pieces : PAGED_MAX_PIECES);
+    c.groups = c.whole ? 0 : (int)pieces;
     c.grid = c.groups > bound ? c.groups : bound;
     return c;
 }

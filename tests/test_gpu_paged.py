@@ -246,6 +246,16 @@ def test_in_place_and_without_stats(dtype):
         _check_attention(c, counts, 4, dtype, "tree", stats=False, max_len=max_len)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("max_len", [10, 5000])
+def test_the_most_query_heads_of_a_kv_head(dtype, max_len):
+    lens, counts = [70, 900], [1, 2]
+    c = Case(23, lens, counts, hd=64, heads=1, page=64)
+    c.put_new(1, counts)
+    _check_attention(c, counts, 1024, dtype, "chain", max_len=max_len)
+    _check_mass(c, counts, 1024, dtype, "chain", max_len=max_len)
+
+
 def test_one_row_each_without_start():
     lens = [5, 700, 0, 64]
     c = Case(2, lens, [1] * 4, hd=64)
@@ -473,6 +483,27 @@ def test_append_as_it_is(dtype):
         _check_append(c, counts, 1, dtype, None, **kw)
         c = Case(8, lens, counts, hd=128, heads=5, page=96)
         _check_append(c, counts, 1, dtype, _rope(128, 0, 0), **kw)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("counts", [[3, 1, 2], [40, 9, 33]])
+def test_append_from_rows_of_their_own(dtype, counts):
+    """Queries, keys and values of different strides, in different tensors: what the same call writes from one."""
+    lens = [5, 0, 31]
+    c, d = (Case(13, lens, counts, hd=64, heads=3) for _ in "cd")
+    rope, n = _rope(64, 1, 0), sum(counts)
+    x, t = _append(c, counts, 2, dtype, rope, None)
+    wide = [torch.full((n, h * 64 + w), 9.0, dtype=TYPES[dtype], device=DEV) for h, w in ((6, 0), (3, 24), (3, 8))]
+    for buf, (a, b) in zip(wide, ((0, 6), (6, 9), (9, 12))):
+        buf[:, :(b - a) * 64] = _dev(x[:, a:b].reshape(n, -1), TYPES[dtype])
+    q = wide[0].unflatten(1, (6, 64))
+    rows = d.g.rows(q, _start(counts))
+    dv.dv_paged_append(d.g.c, 1, rows, rope, 0, wide[1].data_ptr(), wide[1].stride(0), wide[2].data_ptr(), wide[2].stride(0))
+    torch.cuda.synchronize()
+    assert torch.equal(q, t[:, :6])
+    for a, b in zip(c.got(), d.got()):
+        np.testing.assert_array_equal(a, b)
+    assert (wide[1][:, 192:] == 9.0).all() and (wide[2][:, 192:] == 9.0).all()
 
 
 def test_append_a_prompt():
