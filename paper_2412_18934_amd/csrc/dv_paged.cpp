@@ -221,7 +221,7 @@ int64_t dv_paged_attention_workspace(const dv_paged *c, const dv_paged_rows *r)
     int rc = check_cache(c);
     PagedCut cut;
     if (rc || (rc = check_rows(c, r, true)) || (rc = check_scores(r)) || (rc = cut_of(c, r, &cut))) return rc;
-    return (int64_t)paged_attention_bytes(cut, c->head_dim);
+    return (int64_t)paged_attention_bytes(cut, c->n_seqs, c->head_dim);
 }
 
 int dv_paged_attention(const dv_paged *c, int32_t layer, const dv_paged_rows *r, void *out, int64_t out_stride, float *stats,
@@ -238,7 +238,7 @@ int dv_paged_attention(const dv_paged *c, int32_t layer, const dv_paged_rows *r,
     if (!aligned(stats, 8)) return set_err(nullptr, DV_EINVAL, "stats must be 8-byte aligned");
     PagedCut cut;
     if ((rc = cut_of(c, r, &cut))) return rc;
-    const size_t need = paged_attention_bytes(cut, c->head_dim);
+    const size_t need = paged_attention_bytes(cut, c->n_seqs, c->head_dim);
     if (need && (!workspace || !aligned(workspace, 16) || workspace_bytes < 0 || (size_t)workspace_bytes < need))
         return set_err(nullptr, DV_EINVAL, "attention needs a 16-byte aligned workspace of %zu bytes", need);
     PagedAttnArgs a{};
@@ -249,7 +249,10 @@ int dv_paged_attention(const dv_paged *c, int32_t layer, const dv_paged_rows *r,
     a.stats = reinterpret_cast<float2 *>(stats);
     a.groups = cut.groups;
     a.part_o = static_cast<float *>(workspace);
-    if (need) a.part_ml = reinterpret_cast<float2 *>(a.part_o + (size_t)cut.groups * 16 * cut.rt * c->head_dim);
+    if (need) {
+        a.part_ml = reinterpret_cast<float2 *>(a.part_o + (size_t)cut.groups * 16 * cut.rt * c->head_dim);
+        a.line = reinterpret_cast<int2 *>(a.part_ml + (size_t)cut.groups * 16 * cut.rt);
+    }
     return launched(launch_paged_attention(a, r->dtype == DV_BF16, cut, static_cast<hipStream_t>(stream)), "paged attention");
 }
 

@@ -53,6 +53,7 @@ struct PagedAttnArgs {
     int32_t groups;              // workgroups that share all tiles, or 0: one per row block
     float *part_o;               // [groups][16 rt][hd] unnormalised sums
     float2 *part_ml;             // [groups][16 rt]: largest score and sum of weights
+    int2 *line;                  // [n_seqs]: first piece, and pieces of each unit
 };
 
 // How attention is cut.  A unit is a row block (rt row tiles of 16) of a KV head.  Where there are many units, or short
@@ -93,9 +94,9 @@ inline PagedCut paged_cut(int n_seqs, int heads, int group, int n_rows, int max_
     c.grid = c.groups > bound ? c.groups : bound;
     return c;
 }
-inline size_t paged_attention_bytes(const PagedCut &c, int hd)
+inline size_t paged_attention_bytes(const PagedCut &c, int n_seqs, int hd)
 {
-    return c.whole ? 0 : (size_t)c.groups * 16 * c.rt * (hd + 2) * 4;
+    return c.whole ? 0 : (size_t)c.groups * 16 * c.rt * (hd + 2) * 4 + (size_t)n_seqs * 8;
 }
 
 // Mass: a workgroup per sequence and KV head where these are many, else pieces as above.

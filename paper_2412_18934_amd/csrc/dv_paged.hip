@@ -86,21 +86,29 @@ struct Pieces {
         if (c.n_seqs > 64) read(0, bad);
         count();
     }
-    // the lanes come to the 64 sequences among which `reached` holds; false if there are none
-    template <typename F> __device__ __forceinline__ bool seek(F reached, bool &bad)
+    // the lanes come to the next 64 sequences; false if there are none
+    __device__ __forceinline__ bool on(bool &bad)
     {
-        while (!reached()) {
-            if (base + 64 >= c.n_seqs) return false;
-            before = all;
-            read(base + 64, bad);
-            count();
-        }
+        if (base + 64 >= c.n_seqs) return false;
+        before = all;
+        read(base + 64, bad);
+        count();
         return true;
     }
-    // piece number `at`, which is not below those of earlier calls; false if there are not so many
+    // every sequence's first piece, and the pieces of its units
+    __device__ __forceinline__ void publish(int2 *line, bool &bad)
+    {
+        do {
+            const int64_t sum = (int64_t)load.units * cut, first = before + wave_prefix(sum, c.n_seqs - base) - sum;
+            const int i = base + (int)(threadIdx.x & 63);
+            if (i < c.n_seqs) line[i] = make_int2((int)first, cut);
+        } while (on(bad));
+    }
+    // piece number `at`; false if there are not so many
     __device__ __forceinline__ bool take(int64_t at, Segment &x, bool &bad)
     {
-        if (!seek([&] { return at < all; }, bad)) return false;
+        while (at >= all)
+            if (!on(bad)) return false;
         const int64_t sum = (int64_t)load.units * cut, up = before + wave_prefix(sum, c.n_seqs - base);
         const int lane = __builtin_ctzll(__ballot(at < up));
         const int units = __builtin_amdgcn_readlane(load.units, lane), tiles = __builtin_amdgcn_readlane(load.tiles, lane);
@@ -513,8 +521,8 @@ template <bool BF, int HD> __global__ __launch_bounds__(256) void k_paged_append
 //
 // A wave has a tile of its own, so no barrier stands between tiles; K's registers take the next
 // tile when the last row tile's scores are made, V's after the products: up to 128 KB per CU in flight.
-// What bounds it: the pages' bytes.  532 MB of one sequence at 5.75 TB/s (92.6 us with the combining launch of
-// 7), 48 ragged ones (438 MB) at 4.9 TB/s; short calls 2.5 us until a workgroup knows its piece, 3 to 6
+// What bounds it: the pages' bytes.  532 MB of one sequence at 5.8 TB/s (92 us with the combining launch of
+// 6), 48 ragged ones (438 MB) at 4.9 TB/s; short calls 2.5 us until a workgroup knows its piece, 3 to 6
 // until its first tile is there, 2 for the waves' sums.
 // Measured and taken: 4 waves twice per CU for 8 once (93 for 101 us, 48 ragged sequences); V's loads past
 // the caches where a tile is read once (92 for 102, one sequence; K's too: its lines are read in halves, 36 to
@@ -852,15 +860,22 @@ template <int HD, bool BF, int RT, int NW, bool WHOLE> __global__ __launch_bound
             __syncthreads();
         }
     } else {
-        if (piece_at(a.c, a.r, 16 * RT, a.groups, NW, blockIdx.x, x, bad)) segment(x, blockIdx.x);
+        // (the last workgroup writes down for the combining launch how the sequences are cut)
+        if (blockIdx.x == gridDim.x - 1) {
+            Pieces pieces(a.c, a.r, 16 * RT, a.groups, NW, bad);
+            if (wave == 0) pieces.publish(a.line, bad);
+        } else if (piece_at(a.c, a.r, 16 * RT, a.groups, NW, blockIdx.x, x, bad)) {
+            segment(x, blockIdx.x);
+        }
     }
     report(a.c, bad);
 }
 
-// The pieces of a row block combined in a launch of its own.  Workgroup (sequence and KV head, rows):
+// The pieces of a row block combined in a launch of its own (5 to 6 us; 7 where it works out again how the
+// sequences are cut, in place of finding it in the workspace).  Workgroup (sequence and KV head, rows):
 // HD / 4 threads have 4 dims of a row each, and LANES such groups every LANES-th piece; they are
 // combined in LDS.  The order is fixed, so are the results.
-template <int HD, bool BF, int RT, int NW, int LANES> __global__ __launch_bounds__(256) void k_paged_merge(PagedAttnArgs a)
+template <int HD, bool BF, int RT, int LANES> __global__ __launch_bounds__(256) void k_paged_merge(PagedAttnArgs a)
 {
     constexpr int PER = HD / 4, AT_ONCE = 256 / PER / LANES, STEP = LANES == 1 ? 2 : 4;
     __shared__ __align__(16) float sm_o[AT_ONCE][LANES][HD];
@@ -868,14 +883,11 @@ template <int HD, bool BF, int RT, int NW, int LANES> __global__ __launch_bounds
     const int tid = threadIdx.x, s = blockIdx.x / a.c.H, h = blockIdx.x % a.c.H, d0 = 4 * (tid % PER);
     const int part = tid / PER % LANES, mine = tid / PER / LANES;
     bool bad = false;
-    Pieces pieces(a.c, a.r, 16 * RT, a.groups, NW, bad);
-    pieces.seek([&] { return s < pieces.base + 64; }, bad);
-    const int from = s - pieces.base, n = __builtin_amdgcn_readlane(pieces.cut, from);
+    const Seq q = seq_of(a.c, a.r.start, a.r.n_rows, s, PAGED_MAX_NEW, bad);
+    const int2 cut = a.line[s];
+    const int n = cut.y;
     if (n < 2) return;  // (nothing, or one workgroup had it all)
-    const int64_t own = (int64_t)pieces.load.units * pieces.cut;
-    const int64_t before = __shfl((long long)(pieces.before + wave_prefix(own, a.c.n_seqs - pieces.base) - own), from);
-    const Seq q = {__builtin_amdgcn_readlane(pieces.mine.first, from), __builtin_amdgcn_readlane(pieces.mine.n, from),
-                   __builtin_amdgcn_readlane(pieces.mine.len, from)};
+    const int64_t before = cut.x;
     const int rows = q.n * a.r.G, blocks = (rows + 16 * RT - 1) / (16 * RT);
     for (int row0 = blockIdx.y * AT_ONCE; row0 < rows; row0 += gridDim.y * AT_ONCE) {
         const int row = row0 + mine, b = row / (16 * RT), i = row % (16 * RT);
@@ -1405,12 +1417,12 @@ template <int HD, bool BF, int RT, int NW> void attention(const PagedAttnArgs &a
     if (cut.whole) {
         k_paged_attn<HD, BF, RT, NW, true><<<dim3(units, cut.blocks), 64 * NW, 0, s>>>(a);
     } else {
-        k_paged_attn<HD, BF, RT, NW, false><<<(unsigned)cut.grid, 64 * NW, 0, s>>>(a);
+        k_paged_attn<HD, BF, RT, NW, false><<<(unsigned)cut.grid + 1, 64 * NW, 0, s>>>(a);
         // (rows beyond the grid's are looped over)
         auto merge = [&](auto lanes_) {
             constexpr int LANES = decltype(lanes_)::value, AT_ONCE = 256 / (HD / 4) / LANES;
             const int groups = std::min((cut.blocks * 16 * RT + AT_ONCE - 1) / AT_ONCE, 4096);
-            k_paged_merge<HD, BF, RT, NW, LANES><<<dim3(units, groups), 256, 0, s>>>(a);
+            k_paged_merge<HD, BF, RT, LANES><<<dim3(units, groups), 256, 0, s>>>(a);
         };
         // pieces of a unit, about: with many, 8 groups of threads share them
         if (cut.groups > 4 * (int64_t)units * cut.blocks)

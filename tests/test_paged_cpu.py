@@ -208,7 +208,7 @@ uint32_t t_rank(float m) { return rank_of(m); }
 void t_cut(int seqs, int heads, int group, int n_rows, int rows, int len, int cu, int64_t *out)
 {
     const PagedCut c = paged_cut(seqs, heads, group, n_rows, rows, len, cu);
-    out[0] = c.rt, out[1] = c.blocks, out[2] = c.groups, out[3] = c.whole, out[4] = (int64_t)paged_attention_bytes(c, 128);
+    out[0] = c.rt, out[1] = c.blocks, out[2] = c.groups, out[3] = c.whole, out[4] = (int64_t)paged_attention_bytes(c, seqs, 128);
     out[5] = c.grid, out[6] = paged_mass_cut(seqs, heads, len, cu).grid;
 }
 }
@@ -329,4 +329,4 @@ def test_every_row_block_has_a_workgroup(lib, cu):
                         assert whole == (groups == 0) == (size == 0)
                         units = heads * int((-(-rows * group // (16 * rt))).sum())
                         assert grid >= max(units, groups) and mass >= seqs * heads
-                        assert whole or 2 * cu <= groups < 18 * cu and size == groups * 16 * rt * 130 * 4
+                        assert whole or 2 * cu <= groups < 18 * cu and size == groups * 16 * rt * 130 * 4 + 8 * seqs
