@@ -99,14 +99,14 @@ inline size_t paged_attention_bytes(const PagedCut &c, int n_seqs, int hd)
     return c.whole ? 0 : (size_t)c.groups * 16 * c.rt * (hd + 2) * 4 + (size_t)n_seqs * 8;
 }
 
-// Mass: a workgroup per sequence and KV head where these are many, else pieces as above.
+// Mass: a workgroup per sequence and KV head where these are many, else pieces as above, three workgroups per CU.
 struct PagedMassCut {
     bool whole;
     int64_t grid;
 };
 inline PagedMassCut paged_mass_cut(int n_seqs, int heads, int max_len, int n_cu)
 {
-    const int64_t units = (int64_t)n_seqs * heads, slots = 2 * n_cu, most = (units * (max_len / PAGED_TILE + 1) + 7) / 8;
+    const int64_t units = (int64_t)n_seqs * heads, slots = 3 * n_cu, most = (units * (max_len / PAGED_TILE + 1) + 3) / 4;
     const int64_t pieces = most < slots ? most : slots;
     return {units >= 8 * slots || n_seqs > PAGED_MAX_LINE, pieces > units ? pieces : units};
 }

@@ -952,7 +952,8 @@ template <int HD, bool BF, int RT, int LANES> __global__ __launch_bounds__(256) 
 // from K alone, half of what attention read; a tile belongs to one wave, which adds its
 // rows in order, so nothing is atomic.  A tile's masses are asked for with its keys: read where they are added to, they
 // hold up the keys behind them (loads return in order; 29 us for 37 of 16 ragged sequences, 4 rows a KV head).
-// Now 21.8 us for those (80 MB, 3.7 TB/s), 28.6 for two of up to 8191 slots with 16 fp32 rows of 32 heads (98 MB).
+// Now 20.2 us for those (80 MB, 4.0 TB/s), 25.0 for two of up to 8191 slots with 16 fp32 rows of 32 heads (98 MB); with
+// 8 waves a workgroup, of which one fits a CU where rows are fp32, 22.0 and 28.7.
 
 // Sum over the 16 lanes of a row of lanes, in all of them: rotations inside the row
 __device__ __forceinline__ float row_sum(float x)
@@ -968,9 +969,9 @@ __device__ __forceinline__ float row_sum(float x)
     return x;
 }
 
-template <int HD, bool BF> __global__ __launch_bounds__(512) void k_paged_mass(PagedMassArgs a)
+template <int HD, bool BF> __global__ __launch_bounds__(256, 3) void k_paged_mass(PagedMassArgs a)
 {
-    constexpr int NC = HD / 32, NP = BF ? 1 : 3, RT = 4, NW = 8;  // row tiles at a time
+    constexpr int NC = HD / 32, NP = BF ? 1 : 3, RT = 4, NW = 4;  // row tiles at a time
     __shared__ __align__(16) u32x4 qs[RT * NC * NP * 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = lane & 15, g = lane >> 4;
     bool bad = false;
@@ -1462,9 +1463,9 @@ hipError_t launch_paged_attention(const PagedAttnArgs &a, bool bf, const PagedCu
 hipError_t launch_paged_mass(const PagedMassArgs &a, bool bf, hipStream_t s)
 {
     if (a.c.hd == 64)
-        bf ? k_paged_mass<64, true><<<a.groups, 512, 0, s>>>(a) : k_paged_mass<64, false><<<a.groups, 512, 0, s>>>(a);
+        bf ? k_paged_mass<64, true><<<a.groups, 256, 0, s>>>(a) : k_paged_mass<64, false><<<a.groups, 256, 0, s>>>(a);
     else
-        bf ? k_paged_mass<128, true><<<a.groups, 512, 0, s>>>(a) : k_paged_mass<128, false><<<a.groups, 512, 0, s>>>(a);
+        bf ? k_paged_mass<128, true><<<a.groups, 256, 0, s>>>(a) : k_paged_mass<128, false><<<a.groups, 256, 0, s>>>(a);
     return hipGetLastError();
 }
 
