@@ -1280,7 +1280,14 @@ template <int HD, bool RANKS> __global__ __launch_bounds__(512, 4) void k_paged_
     uint16_t *k = a.c.k + base * HD, *v = a.c.v + base * HD;
     const int words = (N + 31) / 32;
     int done = sm_first / 32 * 32;  // (slots before it stay where they are)
-    for (int w0 = done / 32; w0 < words; w0 += MOVE_TILES) {
+    // the next tile from w on with a slot that stays
+    auto from = [&](int w) {
+        uint64_t any = 0;
+        for (; w < words; w += 64)
+            if ((any = __ballot(w + lane < words && sm_bits[min(w + lane, words - 1)] != 0))) return w + (int)__builtin_ctzll(any);
+        return words;
+    };
+    for (int w0 = from(done / 32); w0 < words; w0 = from(w0 + MOVE_TILES)) {
         if (wave == 0) {
             const uint32_t c = lane < MOVE_TILES && w0 + lane < words ? __popc(sm_bits[w0 + lane]) : 0u;
             uint32_t up = c;
