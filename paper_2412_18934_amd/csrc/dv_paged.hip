@@ -1154,8 +1154,8 @@ __global__ __launch_bounds__(256) void k_paged_commit_lens(PagedMoveArgs a)
 // gathered there, 8 slots of a dim to a store.  Source slots increase and each is at least its
 // destination: what a step overwrites is in registers or LDS by then, and no later step's source.
 // What bounds it is that V's tiles are read whole for the slots that stay, and the rate of one CU where heads are few:
-// 128 heads, 2049 slots to 1024 62 us (1.3 MB a workgroup at 26 GB/s, 10 us before the first row moves);
-// 16 ragged sequences of up to 4500 slots to 1500, 64 heads and layers, 406 us (about 1.6 GB).  With V gathered 2 bytes a
+// 128 heads, 2049 slots to 1024 61 us (1.3 MB a workgroup at 26 GB/s, 10 us before the first row moves);
+// 16 ragged sequences of up to 4500 slots to 1500, 64 heads and layers, 389 us (about 1.6 GB).  With V gathered 2 bytes a
 // lane from memory 73 and 460; with ranks read from memory in each of the five passes as well 76 and 528.
 
 constexpr int MOVE_TILES = 24, MOVE = MOVE_TILES * PAGED_TILE, DIMS = 32, V_DIM = 72;  // V_DIM: bytes of a dim's tile in LDS
