@@ -537,11 +537,11 @@ int dv_paged_append(const dv_paged *pg, int32_t layer, const dv_paged_rows *rows
  *   out[r][h] = sum_j softmax_j(z_j) v_j,  z_j = scale q[r][h] . k_j, capped,
  * over the committed slots and the new rows that the mask names.  A row that sees nothing, or nothing but
  * scores of -infinity, gives zeros.  Products are exact (a DV_F32 query enters as three bf16
- * parts), scores, softmax and sums fp32; weights enter with 24 bits (DV_F32) or 16 (DV_BF16, whose
- * output has 8).  Slots that no row of the sequence sees may hold anything, NaN included, and so
- * may new rows for those that do not see them.  Of what a row sees, a key whose score is -infinity has no
- * weight, one whose score is +infinity or NaN makes the row NaN, and an infinity or NaN in a value makes
- * the outputs of its dim infinite or NaN, however small its weight.
+ * parts), scores, softmax and sums fp32; weights enter with all their 24 bits.  Slots that no row of the
+ * sequence sees may hold anything, NaN included, and so may new rows for those that do not see them.  Of
+ * what a row sees, a key whose score is -infinity has no weight, one whose score is +infinity or NaN makes
+ * the row NaN, and an infinity or NaN in a value makes the outputs of its dim infinite or NaN, however
+ * small its weight.
  *   out:   device [n_rows][n_heads][head_dim] of rows->dtype, rows out_stride elements apart, aligned
  *     as q; out may be q with the same stride; they may not overlap otherwise;
  *   stats: device fp32 [n_rows][n_heads][2], or NULL: the largest z of a row and head, and

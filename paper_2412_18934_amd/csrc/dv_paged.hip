@@ -159,20 +159,6 @@ __device__ __forceinline__ void split3(const float *v, u32x4 (&t)[3])
     }
 }
 
-// As two bf16, the second to the nearest: off by at most 2^-17 of the number.
-__device__ __forceinline__ void split2(const float *v, u32x4 (&t)[2])
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const uint32_t a = __float_as_uint(v[2 * i]), b = __float_as_uint(v[2 * i + 1]);
-        t[0][i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
-        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-        const bf16x2 low = {(__bf16)(v[2 * i] - __uint_as_float(a & 0xffff0000u)),
-                            (__bf16)(v[2 * i + 1] - __uint_as_float(b & 0xffff0000u))};
-        t[1][i] = __builtin_bit_cast(uint32_t, low);
-    }
-}
-
 // Eight bf16, infinities and NaN as 0
 __device__ __forceinline__ u32x4 finite(u32x4 x)
 {
@@ -516,8 +502,8 @@ template <bool BF, int HD> __global__ __launch_bounds__(256) void k_paged_append
 //   8 g .. + 8, which are the B operand of O^T = V^T P^T; its D has 4 consecutive dims of
 //   row n.  A row's numbers belong to lanes n + 16 g, only its maximum crosses lanes.
 //
-// Roundings: fp32 queries and weights enter as three bf16 parts (all 24 bits); with bf16 rows the query is one
-// part and a weight two (16 bits: the output keeps 8).  Scores, maxima and sums are fp32.
+// Roundings: weights and fp32 queries enter as three bf16 parts (all 24 bits), bf16 queries as one.  Scores, maxima
+// and sums are fp32.
 //
 // A wave has a tile of its own, so no barrier stands between tiles; K's registers take the next
 // tile when the last row tile's scores are made, V's after the products: up to 128 KB per CU in flight.
@@ -677,7 +663,7 @@ __device__ __forceinline__ void finish(const PagedAttnArgs &a, const Seq &q, int
 
 template <int HD, bool BF, int RT, int NW, bool WHOLE> __global__ __launch_bounds__(64 * NW, 2) void k_paged_attn(PagedAttnArgs a)
 {
-    constexpr int NC = HD / 32, ND = HD / 16, NP = BF ? 1 : 3, NV = BF ? 2 : 3;
+    constexpr int NC = HD / 32, ND = HD / 16, NP = BF ? 1 : 3;
     constexpr int SUMS = NW * 16 * RT * (HD + 4) * 4, PARTS = RT * NC * NP * 1024;
     __shared__ __align__(16) char sm[SUMS > PARTS ? SUMS : PARTS];  // queries, then the waves' sums
     __shared__ float sm_m[NW][16 * RT], sm_l[NW][16 * RT];
@@ -773,13 +759,10 @@ template <int HD, bool BF, int RT, int NW, bool WHOLE> __global__ __launch_bound
                     ps += s8[i];
                 }
                 l_run[rt] += ps;
-                u32x4 p[NV];
-                if constexpr (BF)
-                    split2(s8, p);
-                else
-                    split3(s8, p);
+                u32x4 p[3];
+                split3(s8, p);
 #pragma unroll
-                for (int i = 0; i < NV; ++i)
+                for (int i = 0; i < 3; ++i)
 #pragma unroll
                     for (int dt = 0; dt < ND; ++dt) o[rt][dt] = mfma_bf16(kv.v[dt], p[i], o[rt][dt]);
                 if (!odd) return;
