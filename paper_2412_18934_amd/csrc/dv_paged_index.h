@@ -74,7 +74,7 @@ PAGED_FN int piece_size(int64_t units, int64_t tiles, int most, int least)
 {
     if (units >= most) return 1 << 30;
     const int64_t size = quotient(tiles + most - units - 1, most - units);
-    return size < least ? least : (int)size;
+    return size < least ? least : size > (1 << 30) ? 1 << 30 : (int)size;  // (no unit has more than 2^25 tiles)
 }
 PAGED_FN int pieces_of(int tiles, int size) { return (int)(((uint32_t)tiles + (uint32_t)size - 1) / (uint32_t)size); }
 PAGED_FN int piece_start(int tiles, int pieces, int i) { return (int)((uint64_t)tiles * i / pieces); }
