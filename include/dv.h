@@ -428,9 +428,9 @@ int dv_kvq_commit(dv_handle *h, dv_kvq *kvq, const dv_accept *accept);
  *   lens:  int32 [n_seqs], committed slots of each sequence.
  * All are DEVICE buffers of the caller (k, v and mass 16-byte aligned), read when the kernels
  * run: a captured call follows the table and the lengths.  They need not start at zero.
- * n_heads counts KV heads; head_dim is 64 or 128; page a multiple of 32; n_seqs at most 65536; a
- * sequence has at most table_stride * page slots (2^30 at most); n_pages * n_heads * page is
- * below 2^32.
+ * n_heads counts KV heads; head_dim is 64 or 128; page a multiple of 32; n_layers is at most 65535, n_seqs
+ * 65536; a sequence has at most table_stride * page slots (2^30 at most); n_pages * n_heads * page is
+ * below 2^32, n_heads * n_seqs below 2^22.
  *
  * What stands in device memory is checked there.  A sequence whose numbers cannot be (a
  * negative length, rows outside the call's, more slots than its table row has, a path that does not
@@ -523,7 +523,8 @@ int dv_rope_init(dv_rope *rope);
 
 /* The new rows' queries are turned in place, their keys turned and rounded to bf16 into their
  * slots of layer `layer`, their values rounded to theirs, and the slots' mass is set to 0.  Any
- * number of rows per sequence (a prompt's too).  The committed lengths do not change.
+ * number of rows per sequence (a prompt's too), n_rows * pg->n_heads at most 2^28.  The committed lengths
+ * do not change.
  *   rows: q (or NULL: none), q_stride, start, dtype, n_heads, n_rows;
  *   rope: as dv_rope_init left it, rot_dim at most head_dim, or NULL: nothing is turned;
  *   positions: device int32 [n_rows], or NULL: the slots' numbers;

@@ -12,9 +12,11 @@ namespace {
 
 bool aligned(const void *p, size_t to) { return reinterpret_cast<uintptr_t>(p) % to == 0; }
 
-// A grid's work-items are counted in 32 bits: 2^22 workgroups of 512.
-constexpr int64_t MAX_GROUPS = (1ll << 22) - 1;
-constexpr int MAX_GROUP = 1024, MAX_SEQS = 65536, MAX_ROWS = 1 << 22;
+// A dimension of a grid counts its work-items in 32 bits, so it has less than 2^23 workgroups of 512 (one for each
+// head of a sequence at least) and 2^24 of 256: one for 4 rows of an append, and one for 32 rows of a KV head.  Those
+// of attention and mass stay below that whatever the rows.  Layers are a dimension of their own.
+constexpr int64_t MAX_HEADS = (1ll << 22) - 1, MAX_APPEND = 1ll << 28;  // of all sequences; rows times KV heads
+constexpr int MAX_GROUP = 1024, MAX_SEQS = 65536, MAX_ROWS = 1 << 22, MAX_LAYERS = 65535;
 
 int check_cache(const dv_paged *c)
 {
@@ -23,7 +25,7 @@ int check_cache(const dv_paged *c)
     if (!aligned(c->k, 16) || !aligned(c->v, 16) || !aligned(c->mass, 16) || !aligned(c->table, 4) || !aligned(c->lens, 4) ||
         !aligned(c->fault, 4))
         return set_err(nullptr, DV_EINVAL, "paged cache buffers must be 16-byte aligned (table, lens, fault: 4)");
-    if (c->n_layers < 1 || c->n_heads < 1 || c->n_heads > 65535 || (c->head_dim != 64 && c->head_dim != 128))
+    if (c->n_layers < 1 || c->n_layers > MAX_LAYERS || c->n_heads < 1 || c->n_heads > 65535 || (c->head_dim != 64 && c->head_dim != 128))
         return set_err(nullptr, DV_EINVAL, "bad paged cache shape (%d layers, %d heads, head_dim %d)", c->n_layers, c->n_heads,
                        c->head_dim);
     if (c->page < PAGED_TILE || c->page % PAGED_TILE || c->n_pages < 1 ||
@@ -32,9 +34,8 @@ int check_cache(const dv_paged *c)
                                            "slots of all heads below 2^32", c->n_pages, c->page, c->n_heads);
     if (c->n_seqs < 1 || c->n_seqs > MAX_SEQS || c->table_stride < 1 || (int64_t)c->table_stride * c->page > (1ll << 30))
         return set_err(nullptr, DV_EINVAL, "bad table (%d sequences of %d pages of %d slots)", c->n_seqs, c->table_stride, c->page);
-    if ((int64_t)c->n_layers * c->n_heads * c->n_seqs > MAX_GROUPS)
-        return set_err(nullptr, DV_EINVAL, "paged cache has too many heads (%d layers, %d heads, %d sequences)", c->n_layers,
-                       c->n_heads, c->n_seqs);
+    if ((int64_t)c->n_heads * c->n_seqs > MAX_HEADS)
+        return set_err(nullptr, DV_EINVAL, "paged cache has too many heads (%d of each of %d sequences)", c->n_heads, c->n_seqs);
     return DV_OK;
 }
 
@@ -136,8 +137,6 @@ int cut_of(const dv_paged *c, const dv_paged_rows *r, PagedCut *cut)
     const hipError_t e = current_cus(&n_cu);
     if (e != hipSuccess) return set_err(nullptr, DV_EHIP, "compute units: %s", hipGetErrorString(e));
     *cut = paged_cut(c->n_seqs, c->n_heads, r->n_heads / c->n_heads, r->n_rows, r->max_rows, r->max_len, n_cu);
-    if (cut->grid > MAX_GROUPS || (int64_t)c->n_seqs * c->n_heads * cut->blocks > MAX_GROUPS)
-        return set_err(nullptr, DV_EINVAL, "%d rows of %d heads are too many for one call", r->n_rows, r->n_heads);
     return DV_OK;
 }
 
@@ -184,6 +183,8 @@ int dv_paged_append(const dv_paged *c, int32_t layer, const dv_paged_rows *r, co
     int rc = check_cache(c);
     if (rc || (rc = check_layer(c, layer)) || (rc = check_rows(c, r, false))) return rc;
     if (!k || !v) return set_err(nullptr, DV_EINVAL, "null keys or values");
+    if ((int64_t)r->n_rows * c->n_heads > MAX_APPEND)
+        return set_err(nullptr, DV_EINVAL, "%d rows of %d KV heads are too many for one call", r->n_rows, c->n_heads);
     const int64_t row = (int64_t)c->n_heads * c->head_dim;
     const int size = r->dtype == DV_F32 ? 4 : 2;
     if (!rows_ok(k, k_stride, row, size) || !rows_ok(v, v_stride, row, size))
@@ -193,8 +194,6 @@ int dv_paged_append(const dv_paged *c, int32_t layer, const dv_paged_rows *r, co
         return set_err(nullptr, DV_EINVAL, "rot_dim %d is odd or outside [2, %d]", rope->rot_dim, c->head_dim);
     if (rope && (!(rope->magnitude > 0.) || !std::isfinite((float)rope->magnitude)))
         return set_err(nullptr, DV_EINVAL, "bad magnitude %g", rope->magnitude);
-    if ((int64_t)r->n_rows * ((r->q ? r->n_heads : 0) + 2 * (int64_t)c->n_heads + 32) > 16 * MAX_GROUPS)
-        return set_err(nullptr, DV_EINVAL, "%d rows of %d heads are too many for one call", r->n_rows, r->n_heads);
     PagedAppendArgs a{};
     a.c = view_of(c, layer);
     a.start = r->start;

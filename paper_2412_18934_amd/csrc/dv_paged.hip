@@ -1096,7 +1096,7 @@ template <int HD, int NW> __device__ __forceinline__ void move_rows(const PagedV
 template <int HD, int NW> __global__ __launch_bounds__(64 * NW) void k_paged_commit(PagedMoveArgs a)
 {
     __shared__ uint2 list[PAGED_MAX_NEW];
-    const int h = blockIdx.x % a.c.H, s = blockIdx.x / a.c.H % a.c.n_seqs, layer = blockIdx.x / a.c.H / a.c.n_seqs;
+    const int h = blockIdx.x % a.c.H, s = blockIdx.x / a.c.H, layer = blockIdx.y;
     const int len = a.c.lens[s], n = a.path_len[s], i = threadIdx.x;
     const bool first = h == 0 && layer == 0 && i == 0, apart = a.new_lens != a.c.lens;
     const bool fits = commit_fits(a, s);
@@ -1154,7 +1154,7 @@ template <int HD, bool RANKS> __global__ __launch_bounds__(512, 4) void k_paged_
     __shared__ uint32_t sm_wave[NT / 64], sm_bin, sm_above, sm_word[MOVE_TILES + 1], from_tile[MOVE_TILES], to_tile[MOVE_TILES + 2];
     __shared__ int sm_first;
     uint32_t *hist = reinterpret_cast<uint32_t *>(sm), *ranks = hist + BINS;
-    const int h = blockIdx.x % a.c.H, s = blockIdx.x / a.c.H % a.c.n_seqs, layer = blockIdx.x / a.c.H / a.c.n_seqs;
+    const int h = blockIdx.x % a.c.H, s = blockIdx.x / a.c.H, layer = blockIdx.y;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), N = a.c.lens[s];
     const bool first = h == 0 && layer == 0 && tid == 0, apart = a.new_lens != a.c.lens;
     if (N < 0 || N > (int64_t)a.c.width * a.c.page || N <= a.budget) {
@@ -1462,7 +1462,7 @@ hipError_t launch_paged_mass(const PagedMassArgs &a, bool bf, hipStream_t s)
 hipError_t launch_paged_commit(const PagedMoveArgs &a, hipStream_t s)
 {
     if (a.path) {
-        const unsigned units = (unsigned)a.c.L * a.c.n_seqs * a.c.H;
+        const dim3 units((unsigned)a.c.n_seqs * a.c.H, a.c.L);
         a.c.hd == 64 ? k_paged_commit<64, 2><<<units, 128, 0, s>>>(a) : k_paged_commit<128, 2><<<units, 128, 0, s>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess || a.new_lens != a.c.lens) return e;
@@ -1473,7 +1473,7 @@ hipError_t launch_paged_commit(const PagedMoveArgs &a, hipStream_t s)
 
 hipError_t launch_paged_evict(const PagedMoveArgs &a, hipStream_t s)
 {
-    const unsigned units = (unsigned)a.c.L * a.c.n_seqs * a.c.H;
+    const dim3 units((unsigned)a.c.n_seqs * a.c.H, a.c.L);
     const size_t slots = (size_t)a.c.width * a.c.page;
     if (slots <= PAGED_MAX_RANKS)
         a.c.hd == 64 ? k_paged_evict<64, true><<<units, 512, slots / 8, s>>>(a) : k_paged_evict<128, true><<<units, 512, slots / 8, s>>>(a);

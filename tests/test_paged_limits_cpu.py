@@ -1,8 +1,11 @@
 """Paged cache, host side: the largest numbers that the calls take, and what lies just behind them."""
+import ctypes
+
 import numpy as np
 import pytest
 
-from tests.test_paged_cpu import lib  # noqa: F401 (a fixture)
+from paper_2412_18934_amd import dv
+from tests.test_paged_cpu import A, CALLS, cache, lib, refused, rope, rows  # noqa: F401 (lib: a fixture)
 
 
 @pytest.mark.parametrize("units,most,tiles", [(768, 774, 1 << 25), (1, 2, 1 << 25), (1000, 1001, 1 << 25), (896, 897, 9586981)])
@@ -24,3 +27,52 @@ def test_pieces_fit_where_sizes_are_large(lib):  # noqa: F811
         tiles = int(2.0 ** rng.uniform(18, 25))
         size = lib.t_size(units, units * tiles, most, 4)
         assert size >= 4 and units * lib.t_pieces(tiles, size) <= most
+
+
+# What is refused last shows that all before it was taken: nothing here is launched.
+LAST = dict(
+    append=lambda c: refused(lambda: dv.dv_paged_append(c, 0, rows(n_heads=c.n_heads, q_stride=1 << 24), rope(magnitude=-1.0), 0,
+                                                        A, 1 << 24, A, 1 << 24), "magnitude"),
+    attention=lambda c: refused(lambda: dv.dv_paged_attention(c, 0, rows(n_heads=c.n_heads, q_stride=1 << 24), 0, 1 << 24), "outputs"),
+    mass=lambda c: refused(lambda: dv.dv_paged_mass(c, 0, rows(n_heads=c.n_heads, q_stride=1 << 24), 0), "stats"),
+    commit=lambda c: refused(lambda: dv.dv_paged_commit(c, A, 0, A, A), "path stride"),
+    evict=lambda c: refused(lambda: dv.dv_paged_evict(c, 0, 0, A), "budget"))
+
+
+@pytest.mark.parametrize("call", LAST)
+@pytest.mark.parametrize("kw", [dict(n_layers=32, n_heads=8, n_seqs=65536, table_stride=1), dict(n_layers=65535, n_heads=1, n_seqs=65536),
+                                dict(n_layers=65535, n_heads=63, n_seqs=65536), dict(n_layers=80, n_heads=65535, n_seqs=64)], ids=str)
+def test_many_layers_of_many_sequences_are_taken(call, kw):
+    """n_layers up to 65535, n_heads n_seqs below 2^22, as the header says; not their product."""
+    LAST[call](cache(**kw))
+
+
+@pytest.mark.parametrize("call", CALLS)
+@pytest.mark.parametrize("kw", [dict(n_layers=65536), dict(n_heads=64, n_seqs=65536), dict(n_heads=65535, n_seqs=65)], ids=str)
+def test_more_are_refused(call, kw):
+    refused(lambda: CALLS[call](cache(**kw), rows(n_heads=kw.get("n_heads", 4), q_stride=1 << 24)))
+
+
+@pytest.mark.parametrize("n_rows,heads,ok", [(1 << 22, 64, True), (4096, 65535, True), (1 << 22, 65, False), (4097, 65535, False)])
+def test_the_most_rows_of_an_append(n_rows, heads, ok):
+    """n_rows n_heads up to 2^28."""
+    c, r = cache(n_heads=heads), rows(n_rows=n_rows, n_heads=heads, q_stride=1 << 24)
+    words = "magnitude" if ok else "too many"
+    refused(lambda: dv.dv_paged_append(c, 0, r, rope(magnitude=-1.0), 0, A, 1 << 24, A, 1 << 24), words)
+
+
+def test_attention_needs_no_more_workgroups_than_a_grid_has(lib):  # noqa: F811
+    """Whatever the sequences, heads and rows: grids of 2^24 workgroups of 256 at most, 65535 in the other dimension."""
+    out = (ctypes.c_int64 * 7)()
+    for cu in (1, 64, 256, 512):
+        for seqs in (1, 2, 1000, 1024, 1025, 65536):
+            for heads in (1, 7, 63, 4096, 65535):
+                if seqs * heads >= 1 << 22:
+                    continue
+                for group in (1, 2, 15, 16, 17, 1024):
+                    for n in (1, 2, 16, 63, 64):
+                        for length in (0, 2000, 1 << 30):
+                            lib.t_cut(seqs, heads, group, min(seqs * 64, 1 << 22), n, length, cu, out)
+                            rt, blocks, groups, whole, size, grid, mass = out
+                            assert blocks <= 65535 and mass < 1 << 24
+                            assert whole or (grid + 1 < 1 << 24 and seqs * heads < 1 << 24)
