@@ -28,7 +28,7 @@ struct PagedRowsView {
     int64_t ldq;
     const int32_t *start;
     const uint64_t *mask;
-    float scale, cap;
+    float scale, cap, cap_in[2];  // capped: cap tanh(q.k cap_in[0] cap_in[1])
     int32_t G, n_rows;  // query heads per KV head
 };
 

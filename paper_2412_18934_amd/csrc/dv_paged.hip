@@ -618,9 +618,8 @@ template <int HD, bool BF> __device__ __forceinline__ void scores8(const u32x4 *
 __device__ __forceinline__ void scaled(const PagedRowsView &r, float (&s)[8])
 {
     if (r.cap != 0.f) {
-        const float f = r.scale / r.cap;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) s[i] = r.cap * tanhf(s[i] * f);
+        for (int i = 0; i < 8; ++i) s[i] = r.cap * tanhf(s[i] * r.cap_in[0] * r.cap_in[1]);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) s[i] *= r.scale;
