@@ -169,7 +169,21 @@ class DevicePaged:
 
     def rows(self, q, start=None, mask=None, scale=0.0, cap=0.0, max_rows=1, max_len=None) -> dv.dv_paged_rows:
         """New rows with queries q [n_rows][n_heads][head_dim] (fp32 or bf16; heads and dims without gaps);
-        start, mask: device tensors or None.  The struct keeps the tensors."""
+        start [n_seqs + 1] int32, mask [n_rows] int64 or uint64: device tensors or None.  The struct keeps the
+        tensors."""
+        if q.dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError("queries are fp32 or bf16, not %s" % q.dtype)
+        if q.dim() != 3 or q.shape[2] != self.c.head_dim or q.stride(2) != 1 or (q.shape[1] > 1 and q.stride(1) != q.shape[2]):
+            raise ValueError("queries are [rows][heads][%d], heads and dims without gaps" % self.c.head_dim)
+        if start is None and q.shape[0] != self.c.n_seqs:
+            raise ValueError("%d rows of %d sequences need start" % (q.shape[0], self.c.n_seqs))
+        for name, x, types, n in (("start", start, (torch.int32,), self.c.n_seqs + 1), ("mask", mask, (torch.int64, torch.uint64), q.shape[0])):
+            if x is not None and x.dtype not in types:
+                raise TypeError("%s is %s, not %s" % (name, types[0], x.dtype))
+            if x is not None and (x.shape != (n,) or not x.is_contiguous()):
+                raise ValueError("%s has %d entries without gaps" % (name, n))
+        if any(x is not None and x.device != self.k.device for x in (q, start, mask)):
+            raise ValueError("rows and cache are on one device")
         r = dv.dv_paged_rows(q.data_ptr(), q.stride(0), start.data_ptr() if start is not None else 0,
                              mask.data_ptr() if mask is not None else 0, scale, cap,
                              dv.DV_F32 if q.dtype == torch.float32 else dv.DV_BF16, q.shape[1], q.shape[0], max_rows,

@@ -3,8 +3,9 @@ import ctypes
 
 import numpy as np
 import pytest
+import torch
 
-from paper_2412_18934_amd import dv
+from paper_2412_18934_amd import device, dv
 from tests.test_paged_cpu import A, CALLS, cache, lib, refused, rope, rows  # noqa: F401 (lib: a fixture)
 
 
@@ -76,3 +77,34 @@ def test_attention_needs_no_more_workgroups_than_a_grid_has(lib):  # noqa: F811
                             rt, blocks, groups, whole, size, grid, mass = out
                             assert blocks <= 65535 and mass < 1 << 24
                             assert whole or (grid + 1 < 1 << 24 and seqs * heads < 1 << 24)
+
+
+@pytest.mark.parametrize("change", [
+    dict(q=torch.float16), dict(q=torch.float64), dict(q=torch.int32), dict(start=torch.int64), dict(start=torch.uint8), dict(mask=torch.int32),
+    dict(mask=torch.float64), dict(mask=torch.bool)], ids=str)
+def test_rows_of_other_types_are_refused(change):
+    """By the class that makes the struct of tensors: their addresses alone would be read as the types that the call knows."""
+    g = device.DevicePaged(1, 2, 64, 3, 32, 2, 1, device="cpu")
+    t = dict(q=torch.zeros((3, 4, 64)), start=torch.zeros(3, dtype=torch.int32), mask=torch.zeros(3, dtype=torch.int64))
+    for dtype in (torch.float32, torch.bfloat16):
+        assert g.rows(**dict(t, q=t["q"].to(dtype))).dtype == (dv.DV_F32 if dtype == torch.float32 else dv.DV_BF16)
+    g.rows(**dict(t, mask=t["mask"].to(torch.uint64)))
+    g.rows(t["q"][:2])
+    with pytest.raises(TypeError):
+        g.rows(**dict(t, **{name: t[name].to(dtype) for name, dtype in change.items()}))
+
+
+@pytest.mark.parametrize("change", [
+    lambda t: dict(q=t["q"][0]), lambda t: dict(q=t["q"][:, :, :32]), lambda t: dict(q=torch.zeros((3, 64, 4)).transpose(1, 2)),
+    lambda t: dict(q=torch.zeros((3, 8, 64))[:, ::2]), lambda t: dict(start=t["start"][:2]), lambda t: dict(start=None),
+    lambda t: dict(start=torch.zeros(6, dtype=torch.int32)[::2]), lambda t: dict(mask=t["mask"][:2]),
+    lambda t: dict(mask=torch.zeros(6, dtype=torch.int64)[::2]), lambda t: dict(q=t["q"].to("meta"))])
+def test_rows_of_other_shapes_are_refused(change):
+    """Heads and dims stand behind one another; start and mask have an entry for each sequence and row."""
+    g = device.DevicePaged(1, 2, 64, 3, 32, 2, 1, device="cpu")
+    t = dict(q=torch.zeros((3, 4, 64)), start=torch.zeros(3, dtype=torch.int32), mask=torch.zeros(3, dtype=torch.int64))
+    wide = g.rows(**dict(t, q=torch.zeros((3, 9, 64))[:, 2:6]))
+    assert (wide.q_stride, wide.n_heads, wide.n_rows) == (9 * 64, 4, 3)
+    assert g.rows(**dict(t, q=torch.zeros((3, 2, 64)).expand(3, 2, 64)[:, :1])).n_heads == 1
+    with pytest.raises(ValueError):
+        g.rows(**dict(t, **change(t)))
