@@ -277,10 +277,7 @@ template <bool BF, int HD> __device__ __forceinline__ void append_values(const P
         int s = a.start ? seq_of_row(a.start, a.c.n_seqs, row0) : 0;
         const int row = row0 + tid;
         if (tid < V_ROWS) {
-            if (a.start)
-                while (s < a.c.n_seqs && a.start[s + 1] <= row) ++s;
-            else
-                s = row;
+            s = seq_from(a.start, a.c.n_seqs, s, row);
             sm_row[tid] = NONE;
             if (row < a.n_rows && s < a.c.n_seqs) {
                 const Seq q = seq_of(a.c, a.start, a.n_rows, s, 1 << 30, bad);

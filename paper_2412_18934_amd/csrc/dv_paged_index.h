@@ -51,6 +51,17 @@ PAGED_FN uint32_t row_of(const PagedView &c, int s, int h, int slot, bool &bad)
     return (id * (uint32_t)c.H + (uint32_t)h) * (uint32_t)c.page + ((uint32_t)slot - p * (uint32_t)c.page);
 }
 
+// The sequence that row `row` belongs to, at least s (n_seqs: none), by steps that double and then halve: mostly
+// it is s or near, but any number of empty sequences may lie between.
+PAGED_FN int seq_from(const int32_t *start, int n_seqs, int s, int row)
+{
+    int step = 1;
+    for (; s + step <= n_seqs && start[s + step] <= row; step *= 2) s += step;
+    for (step /= 2; step > 0; step /= 2)
+        if (s + step <= n_seqs && start[s + step] <= row) s += step;
+    return s;
+}
+
 // The work of a call on a sequence: units (KV heads times row blocks of `block` rows), each of
 // them 32-slot tiles.
 struct Load {

@@ -1,11 +1,14 @@
 """Paged cache, host side: the largest numbers that the calls take, and what lies just behind them."""
 import ctypes
+import os
+import subprocess
 
 import numpy as np
 import pytest
 import torch
 
 from paper_2412_18934_amd import device, dv
+from tests.test_engine_cpu import CSRC, ROOT
 from tests.test_paged_cpu import A, CALLS, cache, lib, refused, rope, rows  # noqa: F401 (lib: a fixture)
 
 
@@ -108,3 +111,45 @@ def test_rows_of_other_shapes_are_refused(change):
     assert g.rows(**dict(t, q=torch.zeros((3, 2, 64)).expand(3, 2, 64)[:, :1])).n_heads == 1
     with pytest.raises(ValueError):
         g.rows(**dict(t, **change(t)))
+
+
+STUB = r"""
+#include "dv_paged_index.h"
+extern "C" int t_from(const int32_t *start, int n_seqs, int s, int row) { return seq_from(start, n_seqs, s, row); }
+"""
+
+
+@pytest.fixture(scope="module")
+def search(tmp_path_factory):
+    d = tmp_path_factory.mktemp("search")
+    stub, out = str(d / "stub.cpp"), str(d / "libsearch.so")
+    with open(stub, "w") as f:
+        f.write(STUB)
+    subprocess.run(["g++", "-std=c++17", "-O1", "-Wall", "-shared", "-fPIC", "-fsanitize=undefined", "-fno-sanitize-recover",
+                    "-D__HIP_PLATFORM_AMD__", "-I", "/opt/rocm/include", "-I", os.path.join(ROOT, "include"), "-I", CSRC, stub,
+                    "-o", out], check=True)
+    return ctypes.CDLL(out).t_from
+
+
+@pytest.mark.parametrize("seqs", [1, 2, 3, 63, 64, 65, 1000, 65536])
+def test_the_sequence_of_a_row(search, seqs):
+    """Runs of empty sequences of all lengths, rows before the first and behind the last; whatever sequence the search begins at."""
+    rng = np.random.default_rng(seqs)
+    for empty in (0.0, 0.5, 0.99, 1.0):
+        counts = np.where(rng.random(seqs) < empty, 0, rng.integers(0, 9, seqs))
+        start = np.concatenate([[2], 2 + np.cumsum(counts)]).astype(np.int32)
+        p = start.ctypes.data_as(ctypes.c_void_p)
+        rows_ = np.unique(np.concatenate([rng.integers(0, start[-1] + 2, 50), start[rng.integers(0, seqs + 1, 20)], [0, start[-1], start[-1] + 1]]))
+        for row in rows_.tolist():
+            want = int((start[1:] <= row).sum())
+            for s in {0, want, max(want - 1, 0), int(rng.integers(0, want + 1))}:
+                assert search(p, seqs, s, row) == want
+
+
+def test_starts_that_decrease_lead_nowhere_else(search):
+    rng = np.random.default_rng(5)
+    for _ in range(300):
+        seqs = int(rng.integers(1, 200))
+        start = rng.integers(-2 ** 31, 2 ** 31 - 1, seqs + 1).astype(np.int32)
+        s = int(rng.integers(0, seqs + 1))
+        assert s <= search(start.ctypes.data_as(ctypes.c_void_p), seqs, s, int(rng.integers(0, 1 << 22))) <= seqs
