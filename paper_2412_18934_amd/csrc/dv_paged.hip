@@ -274,7 +274,7 @@ template <bool BF, int HD> __device__ __forceinline__ void append_values(const P
     }
     if (tid < 64) {
         bool bad = false;
-        int s = a.start ? seq_of_row(a.start, a.c.n_seqs, row0) : 0;
+        int s = seq_of_row(a.start, a.c.n_seqs, row0);
         const int row = row0 + tid;
         if (tid < V_ROWS) {
             s = seq_from(a.start, a.c.n_seqs, s, row);
@@ -386,7 +386,7 @@ template <bool BF, int HD> __device__ __forceinline__ void append_rows(const Pag
         uint32_t r = NONE;
         if (row < a.n_rows) {
             int pos = a.positions ? a.positions[row] : 0;
-            const int s = a.start ? seq_of_row(a.start, a.c.n_seqs, row) : row;
+            const int s = seq_of_row(a.start, a.c.n_seqs, row);
             if (s < a.c.n_seqs) {
                 const Seq q = seq_of(a.c, a.start, a.n_rows, s, 1 << 30, bad);
                 own = row >= q.first && row - q.first < q.n;
@@ -427,7 +427,7 @@ template <bool BF, int HD> __device__ __forceinline__ void append_rows(const Pag
     }
 }
 
-// Many rows of a sequence: workgroups of 4 rows' queries and keys, behind them those of 32 rows' values.
+// Many rows of a sequence (so there is a start): workgroups of 4 rows' queries and keys, behind them those of 32 rows' values.
 template <bool BF, int HD> __global__ __launch_bounds__(256) void k_paged_append_rows(PagedAppendArgs a)
 {
     const int groups = (a.n_rows + 3) / 4, b = blockIdx.x - groups;
