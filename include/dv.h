@@ -527,7 +527,8 @@ int dv_rope_init(dv_rope *rope);
  * do not change.
  *   rows: q (or NULL: none), q_stride, start, dtype, n_heads, n_rows;
  *   rope: as dv_rope_init left it, rot_dim at most head_dim, or NULL: nothing is turned;
- *   positions: device int32 [n_rows], or NULL: the slots' numbers;
+ *   positions: device int32 [n_rows], or NULL: the slots' numbers (a sequence that dv_paged_evict has cut down
+ *     has more positions behind it than slots, so its new rows need theirs);
  *   k, v: device [n_rows][pg->n_heads][head_dim] of rows->dtype, rows k_stride and v_stride elements
  *     apart, aligned as q.  q, k and v may be parts of the same rows; their heads may not overlap. */
 int dv_paged_append(const dv_paged *pg, int32_t layer, const dv_paged_rows *rows, const dv_rope *rope,
@@ -576,7 +577,8 @@ int dv_paged_commit(const dv_paged *pg, const int32_t *path, int64_t path_stride
 /* Every sequence of more than `budget` committed slots is cut down to that: in each layer and KV head by itself
  * the last `recent` slots stay, and of the others the budget - recent of largest mass, the
  * lower slot of equal ones (a NaN is larger than all numbers, 0 and -0 are equal).  They move up to slots
- * 0..budget - 1 in their order, with their mass; keys stay turned to the positions that they had.  Slots
+ * 0..budget - 1 in their order, with their mass; keys stay turned to the positions that they had (new rows from
+ * then on are appended with positions, not by slot).  Slots
  * from budget on keep what they hold; their pages are free if nobody else has them.  Needs mass, 1 <=
  * budget, 0 <= recent <= budget, table_stride * page at most 262144.
  *   new_lens: device int32 [n_seqs], set to the smaller of lens and budget (skipped sequences:
