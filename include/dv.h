@@ -438,7 +438,7 @@ int dv_kvq_commit(dv_handle *h, dv_kvq *kvq, const dv_accept *accept);
  * that is not there: its slots are not seen, and what would be written to it is dropped.
  * Either sets *fault (device int32, or NULL) to 1; nothing sets it back.
  *
- * Sequences may share pages that hold a common beginning: attention reads them, and
+ * Sequences may share whole pages of a common beginning: attention reads them, and
  * dv_paged_append and dv_paged_commit write behind the committed slots only.  dv_paged_mass
  * and dv_paged_evict write to all pages of a sequence: there a page stands in one place of the table
  * only. */
@@ -543,7 +543,7 @@ int dv_paged_append(const dv_paged *pg, int32_t layer, const dv_paged_rows *rows
  * sequence sees may hold anything, NaN included, and so may new rows for those that do not see them.  Of
  * what a row sees, a key whose score is -infinity has no weight, one whose score is +infinity or NaN makes
  * the row NaN, and an infinity or NaN in a value makes the outputs of its dim infinite or NaN, however
- * small its weight.
+ * small its weight.  Sums are divided at the end: values times the slots seen have to stay below 2^127.
  *   out:   device [n_rows][n_heads][head_dim] of rows->dtype, rows out_stride elements apart, aligned
  *     as q; out may be q with the same stride; they may not overlap otherwise;
  *   stats: device fp32 [n_rows][n_heads][2], or NULL: the largest z of a row and head, and

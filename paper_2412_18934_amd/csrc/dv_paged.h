@@ -10,7 +10,7 @@
 #define PAGED_TILE 32        // slots of a V tile, and of a step of attention
 #define PAGED_MAX_NEW 64     // new rows of a sequence that a mask names
 #define PAGED_MAX_LINE 1024    // sequences among which a workgroup looks for its piece (64 at a time, about 1 us)
-#define PAGED_MAX_RANKS 10240   // slots of a sequence whose ranks an eviction keeps in LDS
+#define PAGED_MAX_RANKS 10240   // slots of a table row that an eviction keeps the ranks of in LDS
 #define PAGED_MAX_EVICT 262144  // slots of a sequence that an eviction marks in LDS, a bit each
 
 // The cache; layer-wise calls have k, v and mass at their layer.

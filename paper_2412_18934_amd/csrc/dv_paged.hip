@@ -504,9 +504,10 @@ template <bool BF, int HD> __global__ __launch_bounds__(256) void k_paged_append
 //
 // A wave has a tile of its own, so no barrier stands between tiles; K's registers take the next
 // tile when the last row tile's scores are made, V's after the products: up to 128 KB per CU in flight.
-// What bounds it: the pages' bytes.  532 MB of one sequence at 5.8 TB/s (92 us with the combining launch of
-// 6), 48 ragged ones (438 MB) at 4.9 TB/s; short calls 2.5 us until a workgroup knows its piece, 3 to 6
-// until its first tile is there, 2 for the waves' sums.
+// What bounds it: the pages' bytes, once per 16 or 32 rows of a KV head.  532 MB of one sequence 92 us, 5.8 TB/s, 6 of
+// them the combining launch; 48 ragged ones (438 MB) 87 us, 5.0 TB/s, 5 of them that launch; short calls 2.5 us
+// until a workgroup knows its piece, 3 to 6 until its first tile is there, 2 for the waves' sums.  64 rows of a KV
+// head: those 48 143 us, 145 with weights of three parts and not two.
 // Measured and taken: 4 waves twice per CU for 8 once (93 for 101 us, 48 ragged sequences); V's loads past
 // the caches where a tile is read once (92 for 102, one sequence; K's too: its lines are read in halves, 36 to
 // 41 us for eight 16-node trees); queries from LDS and not from 48 registers.
@@ -929,7 +930,8 @@ template <int HD, bool BF, int RT, int LANES> __global__ __launch_bounds__(256) 
 // ---------------------------------------------------------------------------
 // Mass: mass_j += sum over counted rows of exp(z_ij - m_i) / l_i.  The scores are made again
 // from K alone, half of what attention read; a tile belongs to one wave, which adds its
-// rows in order, so nothing is atomic.  A tile's masses are asked for with its keys: read where they are added to, they
+// rows in order, so nothing is atomic.  K and the masses are read again for every 64 rows of a KV head, also for rows
+// that do not count.  A tile's masses are asked for with its keys: read where they are added to, they
 // hold up the keys behind them (loads return in order; 29 us for 37 of 16 ragged sequences, 4 rows a KV head).
 // Now 20.2 us for those (80 MB, 4.0 TB/s), 25.0 for two of up to 8191 slots with 16 fp32 rows of 32 heads (98 MB); with
 // 8 waves a workgroup, of which one fits a CU where rows are fp32, 22.0 and 28.7.
@@ -1037,7 +1039,8 @@ template <int HD, bool BF> __global__ __launch_bounds__(256, 3) void k_paged_mas
 // each is at least its destination; so a wave that always has the same columns of K (or dims of V) can
 // go through the list by itself: what it overwrites is no later row's source, and a step's loads stand before
 // its stores.  What bounds it is V, whose lines hold 32 slots of a dim: five rows of 8 sequences, 40 layers
-// of 40 heads 48 us (63 MB of rows, about 300 of lines), 38 of 16 sequences, 32 of 32, 114 (501 MB, 4.4 TB/s).
+// of 40 heads 48 us (63 MB of rows; counted 115 MB read and 70 written, 3.8 TB/s), 38 of 16 sequences, 32 of 32, 114
+// (501 MB of rows, of which some stay where they are; 247 read and 200 written, 3.9 TB/s).
 // Workgroups are small, so that many wait for their chain of lengths, path, table and rows at once: 4 waves
 // 52 and 112, 8 waves 70 and 124.
 
@@ -1133,9 +1136,9 @@ __global__ __launch_bounds__(256) void k_paged_commit_lens(PagedMoveArgs a)
 // gathered there, 8 slots of a dim to a store.  Source slots increase and each is at least its
 // destination: what a step overwrites is in registers or LDS by then, and no later step's source.
 // What bounds it is that V's tiles are read whole for the slots that stay, and the rate of one CU where heads are few:
-// 128 heads, 2049 slots to 1024 61 us (1.3 MB a workgroup at 26 GB/s, 10 us before the first row moves);
-// 16 ragged sequences of up to 4500 slots to 1500, 64 heads and layers, 389 us (about 1.6 GB).  With V gathered 2 bytes a
-// lane from memory 73 and 460; with ranks read from memory in each of the five passes as well 76 and 528.
+// 128 heads, 2049 slots to 1024 63 us (1.35 MB a workgroup at 25 GB/s, 10 us before the first row moves);
+// 16 ragged sequences of up to 4500 slots to 1500, 64 heads and layers, 389 us (counted 0.93 GB read and 0.61 written,
+// 4.0 TB/s).  With V gathered 2 bytes a lane from memory 73 and 460.
 
 constexpr int MOVE_TILES = 24, MOVE = MOVE_TILES * PAGED_TILE, DIMS = 32, V_DIM = 72;  // V_DIM: bytes of a dim's tile in LDS
 
@@ -1470,6 +1473,10 @@ hipError_t launch_paged_commit(const PagedMoveArgs &a, hipStream_t s)
 hipError_t launch_paged_evict(const PagedMoveArgs &a, hipStream_t s)
 {
     const dim3 units((unsigned)a.c.n_seqs * a.c.H, a.c.L);
+    // Ranks are in LDS where all slots of a table row fit; else every pass reads them from memory by way of the table,
+    // for short sequences in wide tables too: 66 for 62 us (2049 slots to 1024 in tables of 10368 and 10240),
+    // 412 for 389 (16 ragged sequences of up to 4500, tables of 10304 and 10240), 276 for 256 (9000 to 4500).  Widest
+    // tables leave room for one workgroup per CU: 449.
     const size_t slots = (size_t)a.c.width * a.c.page;
     if (slots <= PAGED_MAX_RANKS)
         a.c.hd == 64 ? k_paged_evict<64, true><<<units, 512, slots / 8, s>>>(a) : k_paged_evict<128, true><<<units, 512, slots / 8, s>>>(a);
