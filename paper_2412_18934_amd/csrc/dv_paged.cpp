@@ -113,11 +113,12 @@ PagedRowsView view_of(const dv_paged *c, const dv_paged_rows *r)
     v.cap = r->cap;
     if (r->cap != 0.f) {
         // scale / cap; a factor that is too large is the largest number (a product of 0 stays 0), one that is too
-        // small to have all its bits comes in two
+        // small to have all its bits comes in two halves, of which the first is a power of 2
         const double f = (double)v.scale / r->cap, most = std::numeric_limits<float>::max();
         const bool small = std::fabs(f) < std::numeric_limits<float>::min();
-        v.cap_in[0] = small ? 0x1p-64f : (float)std::fmax(-most, std::fmin(f, most));
-        v.cap_in[1] = small ? (float)(f * 0x1p64) : 1.f;
+        const double half = small ? std::exp2(std::floor(std::log2(std::fabs(f)) / 2)) : 1.;
+        v.cap_in[0] = small ? (float)half : (float)std::fmax(-most, std::fmin(f, most));
+        v.cap_in[1] = small ? (float)(f / half) : 1.f;
     }
     v.G = r->n_heads / c->n_heads;
     v.n_rows = r->n_rows;

@@ -13,7 +13,7 @@ from tests.test_gpu_paged import Case, _check_attention, _check_mass, _queries  
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("cap,scale,std", [(3e38, 0.0, 1.3), (3e38, 1e-4, 500.0), (1e30, 1e-12, 3e9), (1e10, 0.0, 1.0), (1e-38, 0.0, 1.0),
+@pytest.mark.parametrize("cap,scale,std", [(3e38, 0.0, 1.3), (3e38, 1e-4, 500.0), (3e38, 1e-20, 3e18), (3e38, 1e-37, 3e35), (1e30, 1e-12, 3e9), (1e10, 0.0, 1.0), (1e-38, 0.0, 1.0),
                                            (1e-40, 0.5, 1.0)])
 def test_caps_at_the_ends(dtype, cap, scale, std):
     """scale / cap is no number of 32 bits there: less than the smallest, or larger than all."""
