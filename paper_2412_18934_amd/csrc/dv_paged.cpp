@@ -178,8 +178,13 @@ int dv_rope_init(dv_rope *r)
         if (r->scaling == DV_ROPE_LINEAR) f /= r->factor;
         if (turns || log_turns) {
             const double t = r->original_ctx * f / (2. * M_PI);
-            double w = turns ? (t - r->low) / (r->high - r->low) : std::log(t / r->low) / std::log(r->high / r->low);
-            w = w < 0. ? 0. : w > 1. ? 1. : w;
+            // (bounds far apart have no quotient, those close together one logarithm)
+            const double w = t <= r->low    ? 0.
+                             : t >= r->high ? 1.
+                             : turns        ? (t - r->low) / (r->high - r->low)
+                             : r->high > 2. * r->low
+                                 ? (std::log(t) - std::log(r->low)) / (std::log(r->high) - std::log(r->low))
+                                 : std::log1p((t - r->low) / r->low) / std::log1p((r->high - r->low) / r->low);
             f *= w + (1. - w) / r->factor;
         }
         r->freq[i] = f;

@@ -1,5 +1,6 @@
 """Paged cache, host side: the largest numbers that the calls take, and what lies just behind them."""
 import ctypes
+import math
 import os
 import subprocess
 
@@ -153,3 +154,19 @@ def test_starts_that_decrease_lead_nowhere_else(search):
         start = rng.integers(-2 ** 31, 2 ** 31 - 1, seqs + 1).astype(np.int32)
         s = int(rng.integers(0, seqs + 1))
         assert s <= search(start.ctypes.data_as(ctypes.c_void_p), seqs, s, int(rng.integers(0, 1 << 22))) <= seqs
+
+
+@pytest.mark.parametrize("low,high", [(1e-320, 1.0), (5e-324, 1e-300), (1e-300, 1e300), (1e-310, 1e308), (1.0, 1.0 + 2.0 ** -52),
+                                      (np.nextafter(2.0, 0), 2.0), (np.nextafter(2.0, 0) * 2.0 ** 9, 2.0 ** 10)], ids=str)
+@pytest.mark.parametrize("scaling", [dv.DV_ROPE_TURNS, dv.DV_ROPE_LOG_TURNS])
+def test_frequencies_between_bounds_of_all_sizes(low, high, scaling):
+    """Every pair's is between f / factor and f, whose turns are past the bounds at one of them; also between bounds that a
+    quotient cannot hold, or the logarithm not tell apart."""
+    r = rope(scaling=scaling, low=float(low), high=float(high), original_ctx=2 ** 30)
+    f = np.array([r.base ** (-2 * i / 64) for i in range(32)])
+    dv.dv_rope_init(r)
+    got, t = np.array(list(r.freq)[:32]), 2 ** 30 * f / (2 * math.pi)
+    assert np.isfinite(got).all()
+    assert (got >= f / 8 * (1 - 1e-14)).all() and (got <= f * (1 + 1e-14)).all()
+    np.testing.assert_allclose(got[t >= high], f[t >= high], rtol=1e-14)
+    np.testing.assert_allclose(got[t <= low], f[t <= low] / 8, rtol=1e-14)
